@@ -509,6 +509,150 @@ int janus_grouped_gemm_noalloc(const float* A, const float* B, float* C, const i
 int32_t janus_wgrad_chunk_rows(int64_t M, int32_t P, int32_t Q);
 
 /*
+ * Operators around an expert block
+ * --------------------------------
+ * What a block h <- h + MoE(h) needs next to its grouped products: the norms before and
+ * after it with its gate and residual scale, the whole expert layer for a few tokens, and
+ * activations held in 8 bits between the forward and the backward pass.  All of them take no
+ * context and allocate nothing: scratch memory is the caller's (`work`, 16-byte aligned, of at
+ * least the bytes that the *_workspace function of the same arguments gives; its contents
+ * need no preparation and mean nothing afterwards), so calls on different streams and captured
+ * graphs are independent as long as they use different scratch memory and outputs.  They run on
+ * the current device, read nothing on the host and can be captured into a graph.
+ *
+ * Arrays are row-major with a distance of ld* elements between rows (at least their width;
+ * checked).  Element types are those of janus_type; sums, statistics and everything between
+ * input and output are held in fp32, and outputs are rounded once (to nearest, ties to even).
+ * Every address is a multiple of its element's size.  Where all rows start on multiples of 16
+ * bytes (packed values: see there) and widths are multiples of 16 bytes, loads and stores are
+ * 16 bytes wide; other layouts give the same results more slowly.  No kernel uses atomics on
+ * floating-point values; results are the same on every run.
+ */
+typedef enum janus_type { JANUS_F32 = 0, JANUS_BF16 = 1, JANUS_F16 = 2 } janus_type;
+typedef enum janus_act { JANUS_ACT_NONE = 0, JANUS_ACT_SILU = 1 } janus_act;
+
+/*
+ * The norms on both sides of a residual update, with its gate and residual scale:
+ *   u = w_post * b / rms(b)        (u = b without w_post)
+ *   r = x + scale * gate * u       (factors that are NULL are 1)
+ *   n = w_pre * r / rms(r)         (not formed without w_pre)
+ * with rms(v) = sqrt(mean(v^2) + eps), the mean over the d columns of a row.
+ *   rows      rows of every array (>= 0, below 2^31)
+ *   d         width, 1..8192 (wider: JANUS_EUNSUPPORTED)
+ *   type      janus_type of x, b, r, n, the gate and their gradients
+ *   eps       >= 0
+ *   w_post, scale, w_pre  [d] fp32, or NULL
+ *   gate      NULL; [rows, d] (one gate per row) with gate_off NULL; or [n_seq, d], one
+ *             gate per sequence (structure), with
+ *   gate_off  [n_seq + 1] int32 on the device: sequence s holds the rows gate_off[s] ..
+ *             gate_off[s + 1] - 1; non-decreasing, gate_off[0] = 0, gate_off[n_seq] <= rows.
+ *             Rows from gate_off[n_seq] on belong to no sequence: nothing of them is read,
+ *             written or added to a gradient.  Offsets that break these rules give wrong
+ *             values but no access outside the arrays.
+ */
+typedef struct janus_norm {
+  int64_t rows;
+  int32_t d;
+  int32_t type;
+  float eps;
+  int32_t n_seq;
+  const float* w_post;
+  const float* scale;
+  const float* w_pre;
+  const void* gate;
+  int64_t ldg;
+  const int32_t* gate_off;
+} janus_norm;
+
+/* Forward: r and, with w_pre, n (else n is NULL).  n is taken from r before r is rounded.  r may
+ * be x and n may be b (same pointer and row distance); other overlaps are not allowed.
+ * Errors: JANUS_EINVAL, JANUS_EUNSUPPORTED, JANUS_EHIP. */
+int janus_residual_norm(const janus_norm* p /* host */, const void* x, int64_t ldx, const void* b, int64_t ldb,
+                        void* r, int64_t ldr, void* n, int64_t ldn, void* stream);
+
+/*
+ * Backward, at the stored r and b (the statistics are taken from them again): from dr (NULL:
+ * zero) and dn, the gradients in r and n (dn and r NULL without w_pre), the gradients dx and db and,
+ * where the pointer is not NULL, dw_post, dscale, dw_pre [d] fp32 and dgate (type, the
+ * gate's shape, rows lddg apart; a sequence without rows gets zeros).  dx may be dr and db may be dn.
+ * Gradients of parameters that p does not have must be NULL.
+ */
+int64_t janus_residual_norm_grad_workspace(const janus_norm* p /* host */);
+int janus_residual_norm_grad(const janus_norm* p /* host */, const void* dr, int64_t lddr, const void* dn,
+                             int64_t lddn, const void* r, int64_t ldr, const void* b, int64_t ldb, void* dx,
+                             int64_t lddx, void* db, int64_t lddb, float* dw_post, float* dscale, float* dw_pre,
+                             void* dgate, int64_t lddg, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * A whole expert layer for a few tokens (1..64), with the conventions of the training step's
+ * layers: l = x router + beta in fp32, the top_k largest logits of a token (descending, lower
+ * index first on ties), gates the softmax probabilities of the chosen (normalize = 1: divided by
+ * their sum), y = sum_c g_c W_down^T SiLU(W_up^T x) of the chosen experts.
+ *   d, d_hidden  widths, multiples of 16, at most 16384 and 65536
+ *   n_experts    1..256;  top_k 1..min(n_experts, 8)
+ *   type         janus_type of x, y, w_up and w_down
+ *   router       [d, n_experts] fp32;  beta [n_experts] fp32 or NULL (-inf masks an expert out)
+ *   w_up         [n_experts, d, d_hidden];  w_down [n_experts, d_hidden, d]; 16-byte aligned
+ * x and y need rows that start on 16 bytes.  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
+ * [tokens, top_k] fp32.  A token whose logits are all -inf gets gates of zero and y = 0; one with
+ * a NaN logit gets gates and y of NaN.  Neither reaches other tokens.  The choice is exact up to the fp32
+ * rounding of the logits.  y may not overlap x.
+ * Errors: JANUS_EINVAL (also misaligned arrays), JANUS_EUNSUPPORTED (sizes beyond these), JANUS_EHIP.
+ */
+typedef struct janus_experts {
+  int32_t d;
+  int32_t d_hidden;
+  int32_t n_experts;
+  int32_t top_k;
+  int32_t type;
+  int32_t normalize;
+  const float* router;
+  const float* beta;
+  const void* w_up;
+  const void* w_down;
+} janus_experts;
+
+int64_t janus_expert_layer_workspace(const janus_experts* p /* host */, int32_t tokens);
+int janus_expert_layer(const janus_experts* p /* host */, const void* x, int64_t ldx, int32_t tokens, void* y,
+                       int64_t ldy, int32_t* eid, float* gate, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * Activations in 8 bits.  The columns of a row are cut into blocks of 32; a block holds int8
+ * values q and one code byte c and stands for q 2^(c - 127).  The power of two is the least with
+ * max|x| <= 127 2^(c - 127), but not below 2^-126; values are rounded to nearest, ties to even, so
+ * each is off by at most max|x| / 127 of its block.  A block with an infinity or NaN gets c = 255
+ * and q = 0 and reads as NaN.
+ *   q [rows, d] int8, rows ldq apart;  code [rows, ceil(d / 32)] uint8, rows ldc apart.
+ * Rows of q that start on multiples of 16 bytes are read and written fastest.  Columns of q between d and ldq are neither read
+ * into a result nor written.
+ */
+int janus_pack_rows(const void* x, int64_t ldx, int32_t type, int64_t rows, int32_t d, int8_t* q, int64_t ldq,
+                    uint8_t* code, int64_t ldc, void* stream);
+
+/*
+ * What packed rows stand for, in `type`.  act JANUS_ACT_NONE: value = X (grad and out NULL).
+ * JANUS_ACT_SILU, X being stored pre-activations: value = SiLU(X) and out = grad * SiLU'(X); either
+ * value or the pair grad, out may be NULL.  out may be grad.
+ */
+int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t ldc, int64_t rows, int32_t d,
+                      int32_t type, int32_t act, const void* grad, int64_t ldg, void* out, int64_t ldo, void* value,
+                      int64_t ldv, void* stream);
+
+/*
+ * janus_grouped_wgrad that reads its left operand in 8 bits:
+ *   G_g[p, c] = sum over the rows m of group g of X[m, p] B[m, c]
+ * with X packed [rows, P], B [rows, Q] of `type`, G [n_groups, P, Q] fp32 and row_off [n_groups + 1]
+ * int32 on the device, non-decreasing from 0 (row_off[n_groups] <= rows: rows behind the last group are not
+ * read).  1..1024 groups; groups without rows get zeros.  Every product is exact in fp32, sums are held in
+ * fp32 and split over row chunks that are added in a fixed order.  Offsets that break these rules
+ * give wrong values but no access outside the arrays.
+ */
+int64_t janus_packed_wgrad_workspace(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type);
+int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t ldc, const void* B, int64_t ldb,
+                       int32_t type, float* G, const int32_t* row_off, int32_t n_groups, int64_t rows, int32_t P,
+                       int32_t Q, void* work, int64_t work_bytes, void* stream);
+
+/*
  * Optional profiler of the kernel families of janus_build_edges and
  * janus_step (host-side bookkeeping; HIP events recorded on the caller's
  * stream around each family of launches).

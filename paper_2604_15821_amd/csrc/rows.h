@@ -1,0 +1,80 @@
+// Row-wise access to fp32, bf16 and fp16 arrays, shared by the operators around an expert block.
+#pragma once
+
+#include <climits>
+
+#include "common.h"
+
+namespace janus {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// N consecutive values as fp32.  The address is a multiple of their size, at most of 16 bytes.
+// Stores round to nearest, ties to even.
+template <typename T, int N>
+__device__ __forceinline__ void load_run(const T* __restrict__ p, float* v) {
+  constexpr int kBytes = sizeof(T) * N;
+  typedef T vec __attribute__((ext_vector_type(N)));
+  if constexpr (N == 1) {
+    v[0] = (float)p[0];
+  } else if constexpr (kBytes <= 16) {
+    const vec u = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = (float)u[j];
+  } else {
+    load_run<T, N / 2>(p, v);
+    load_run<T, N / 2>(p + N / 2, v + N / 2);
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_run(T* __restrict__ p, const float* v) {
+  constexpr int kBytes = sizeof(T) * N;
+  typedef T vec __attribute__((ext_vector_type(N)));
+  if constexpr (N == 1) {
+    p[0] = (T)v[0];
+  } else if constexpr (kBytes <= 16) {
+    vec u;
+#pragma unroll
+    for (int j = 0; j < N; ++j) u[j] = (T)v[j];
+    *reinterpret_cast<vec*>(p) = u;
+  } else {
+    store_run<T, N / 2>(p, v);
+    store_run<T, N / 2>(p + N / 2, v + N / 2);
+  }
+}
+
+// Sum over the 16 lanes of a DPP row, in every lane of it.
+__device__ __forceinline__ float row16_sum(float v) {
+  v = dpp_step<0xB1>(v);    // quad_perm(1, 0, 3, 2)
+  v = dpp_step<0x4E>(v);    // quad_perm(2, 3, 0, 1)
+  v = dpp_step<0x141>(v);   // row_half_mirror
+  return dpp_step<0x140>(v);   // row_mirror
+}
+
+inline bool type_known(int t) { return t == JANUS_F32 || t == JANUS_BF16 || t == JANUS_F16; }
+inline int type_bytes(int t) { return t == JANUS_F32 ? 4 : 2; }
+
+// Runs f with a value of the element type that `type` names.
+template <typename F>
+inline void with_type(int type, F f) {
+  if (type == JANUS_F32) f(float{});
+  else if (type == JANUS_BF16) f(__bf16{});
+  else f(_Float16{});
+}
+
+// Whether every row of `ld` elements starts on a multiple of `align` bytes (null arrays do).
+inline bool rows_aligned(const void* p, int64_t ld, int elem, int align = 16) {
+  return !p || ((reinterpret_cast<uintptr_t>(p) % align) == 0 && (ld * elem) % align == 0);
+}
+
+// The last launch's error, as a return code.
+inline int launched() {
+  JANUS_HIP_TRY(hipGetLastError());
+  return JANUS_OK;
+}
+
+}  // namespace janus

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 
@@ -49,6 +50,18 @@ class Edges(C.Structure):
 
 class Labels(C.Structure):
     _fields_ = [("task", C.c_void_p), ("charge", C.c_void_p), ("spin", C.c_void_p)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int32), ("type", C.c_int32), ("eps", C.c_float), ("n_seq", C.c_int32),
+                ("w_post", C.c_void_p), ("scale", C.c_void_p), ("w_pre", C.c_void_p), ("gate", C.c_void_p),
+                ("ldg", C.c_int64), ("gate_off", C.c_void_p)]
+
+
+class Experts(C.Structure):
+    _fields_ = [("d", C.c_int32), ("d_hidden", C.c_int32), ("n_experts", C.c_int32), ("top_k", C.c_int32),
+                ("type", C.c_int32), ("normalize", C.c_int32), ("router", C.c_void_p), ("beta", C.c_void_p),
+                ("w_up", C.c_void_p), ("w_down", C.c_void_p)]
 
 
 class ProfileEntry(C.Structure):
@@ -98,6 +111,19 @@ def _lib():
         lib.janus_grouped_gemm_noalloc.argtypes = [vp, vp, vp, vp, i32, i64, i32, i32, i32, vp]
         lib.janus_wgrad_chunk_rows.argtypes = [i64, i32, i32]
         lib.janus_wgrad_chunk_rows.restype = i32
+        lib.janus_residual_norm.argtypes = [C.POINTER(Norm), vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        lib.janus_residual_norm_grad_workspace.argtypes = [C.POINTER(Norm)]
+        lib.janus_residual_norm_grad_workspace.restype = i64
+        lib.janus_residual_norm_grad.argtypes = [C.POINTER(Norm), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                                 vp, vp, vp, vp, i64, vp, i64, vp]
+        lib.janus_expert_layer_workspace.argtypes = [C.POINTER(Experts), i32]
+        lib.janus_expert_layer_workspace.restype = i64
+        lib.janus_expert_layer.argtypes = [C.POINTER(Experts), vp, i64, i32, vp, i64, vp, vp, vp, i64, vp]
+        lib.janus_pack_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, i64, vp]
+        lib.janus_unpack_rows.argtypes = [vp, i64, vp, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+        lib.janus_packed_wgrad_workspace.argtypes = [i64, i32, i32, i32, i32]
+        lib.janus_packed_wgrad_workspace.restype = i64
+        lib.janus_packed_wgrad.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i64, i32, i32, vp, i64, vp]
         lib.janus_set_workspace_limit.argtypes = [vp, i64]
         lib.janus_set_concurrency.argtypes = [vp, C.c_int]
         lib.janus_set_edge_builder.argtypes = [vp, C.c_int32]
@@ -116,6 +142,9 @@ def exported_symbols():
     names = ["janus_create", "janus_destroy", "janus_weight_layout", "janus_build_edges", "janus_step",
              "janus_step_stress", "janus_step_ex", "janus_step_pos",
              "janus_grouped_gemm", "janus_grouped_gemm_noalloc", "janus_grouped_wgrad", "janus_wgrad_chunk_rows",
+             "janus_residual_norm", "janus_residual_norm_grad", "janus_residual_norm_grad_workspace",
+             "janus_expert_layer", "janus_expert_layer_workspace", "janus_pack_rows", "janus_unpack_rows",
+             "janus_packed_wgrad", "janus_packed_wgrad_workspace",
              "janus_profile_enable",
              "janus_profile_read",
              "janus_set_workspace_limit", "janus_set_concurrency", "janus_set_edge_builder", "janus_last_chunks",
@@ -489,6 +518,308 @@ def grouped_gemm_noalloc(A, B, row_off, K, N, trans_b, out):
                                            _stream())
     if rc:
         raise JanusError(rc, "janus_grouped_gemm_noalloc")
+    return out
+
+
+# ------------------------------------------------------- operators around an expert block
+
+ACT = {"none": 0, "silu": 1}
+
+
+def _types():
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _type_of(t, name):
+    """janus_type of a tensor or of a torch dtype."""
+    import torch
+    dt = t.dtype if isinstance(t, torch.Tensor) else t
+    code = _types().get(dt)
+    if code is None:
+        raise TypeError(f"{name}: {dt}, expected float32, bfloat16 or float16")
+    return code
+
+
+def _rows(t, name, dtype, shape, device):
+    """Check a [rows, width] tensor whose rows may lie apart; returns (address, row distance)."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected a device tensor on {device}")
+    n, w = shape
+    if n == 0 or w == 0:
+        return 0, w
+    ld, step = t.stride()
+    if step != 1 and w > 1:
+        raise ValueError(f"{name}: the values of a row must lie next to each other")
+    if n == 1:
+        ld = w
+    if ld < w:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), ld
+
+
+def _param(t, name, d, device):
+    """Address of an optional fp32 parameter vector of d values (None: NULL)."""
+    return None if t is None else _arg(t, name, "f32", (d,), device).data_ptr()
+
+
+def _matrix(t, name):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected two dimensions")
+    return t.shape[0], t.shape[1], t.device
+
+
+class _on:
+    """The device of the tensors is current within (a switch only where it is not yet); gives its
+    current stream, on which the call runs."""
+
+    def __init__(self, device):
+        self.device, self.guard = device, None
+
+    def __enter__(self):
+        import torch
+        if torch.cuda.current_device() != self.device.index:
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *e):
+        if self.guard is not None:
+            self.guard.__exit__(*e)
+
+
+def _call(rc, where):
+    if rc < 0:
+        raise JanusError(rc, where)
+    return rc
+
+
+def _norm(rows, d, like, device, w_post, gate, gate_off, scale, w_pre, eps):
+    p = Norm(rows, d, _type_of(like, "b"), float(eps), 0, _param(w_post, "w_post", d, device),
+             _param(scale, "scale", d, device), _param(w_pre, "w_pre", d, device), None, d, None)
+    if gate_off is not None:
+        if gate is None:
+            raise ValueError("gate_off: without a gate")
+        _arg(gate_off, "gate_off", "i32", (None,), device)
+        p.n_seq = gate_off.shape[0] - 1
+        if p.n_seq < 0:
+            raise ValueError("gate_off: needs at least one offset")
+        p.gate_off = gate_off.data_ptr()
+    if gate is not None:
+        p.gate, p.ldg = _rows(gate, "gate", like.dtype, (rows if gate_off is None else p.n_seq, d), device)
+        # a gate without rows has no address and is never read, but has to be told from none
+        p.gate = p.gate or (gate_off if gate_off is not None else w_post if w_post is not None else like).data_ptr() or 16
+    return p
+
+
+def residual_norm(x, b, w_post=None, gate=None, gate_off=None, scale=None, w_pre=None, eps=1e-6, out=None):
+    """The norms after and before a block, with its gate and residual scale:
+
+        u = w_post * b / rms(b),   r = x + scale * gate * u,   n = w_pre * r / rms(r)
+
+    x, b [rows, d] float32, bfloat16 or float16 device tensors (rows may lie apart); w_post, scale
+    and w_pre [d] float32 or None; gate None, [rows, d], or one row per sequence [n_seq, d] with gate_off
+    [n_seq + 1] int32 (rows behind the last sequence are left alone: zero in new outputs, as they
+    were in `out`).  Returns (r, n), n None without w_pre; out = (r, n) to write into, where r may be x and
+    n may be b."""
+    import torch
+    rows, d, dev = _matrix(b, "b")
+    pb, ldb = _rows(b, "b", b.dtype, (rows, d), dev)
+    px, ldx = _rows(x, "x", b.dtype, (rows, d), dev)
+    p = _norm(rows, d, b, dev, w_post, gate, gate_off, scale, w_pre, eps)
+    if out is None:
+        new = torch.empty if gate_off is None else torch.zeros
+        r = new(rows, d, dtype=b.dtype, device=dev)
+        n = None if w_pre is None else new(rows, d, dtype=b.dtype, device=dev)
+    else:
+        r, n = out
+        if (n is None) != (w_pre is None):
+            raise ValueError("out: n is given exactly where w_pre is")
+    pr, ldr = _rows(r, "r", b.dtype, (rows, d), dev)
+    pn, ldn = (None, 0) if n is None else _rows(n, "n", b.dtype, (rows, d), dev)
+    with _on(dev) as stream:
+        _call(_lib().janus_residual_norm(C.byref(p), px, ldx, pb, ldb, pr, ldr, pn, ldn, stream), "janus_residual_norm")
+    return r, n
+
+
+class NormGrads(NamedTuple):
+    """Gradients of residual_norm; None where the forward pass had no such input."""
+    dx: object
+    db: object
+    dw_post: object
+    dgate: object
+    dscale: object
+    dw_pre: object
+
+
+def residual_norm_grad(dr, dn, r, b, w_post=None, gate=None, gate_off=None, scale=None, w_pre=None, eps=1e-6, out=None):
+    """Gradients of residual_norm in all its inputs, at the stored r and b, from the gradients dr and
+    dn of its outputs (dr None: zero; dn and r None without w_pre).  out = (dx, db) to write into, where
+    dx may be dr and db may be dn.  Rows behind the last sequence add to no gradient."""
+    import torch
+    rows, d, dev = _matrix(b, "b")
+    dt = b.dtype
+    like = lambda t, name: (None, 0) if t is None else _rows(t, name, dt, (rows, d), dev)  # noqa: E731
+    pb, ldb = _rows(b, "b", dt, (rows, d), dev)
+    p = _norm(rows, d, b, dev, w_post, gate, gate_off, scale, w_pre, eps)
+    if w_pre is not None and (dn is None or r is None):
+        raise ValueError("dn, r: required with w_pre")
+    if w_pre is None and dn is not None:
+        raise ValueError("dn: without w_pre")
+    pdr, lddr = like(dr, "dr")
+    pdn, lddn = like(dn, "dn")
+    pr, ldr = like(r, "r")
+    if out is None:
+        new = torch.empty if gate_off is None else torch.zeros
+        dx, db = new(rows, d, dtype=dt, device=dev), new(rows, d, dtype=dt, device=dev)
+    else:
+        dx, db = out
+    pdx, lddx = _rows(dx, "dx", dt, (rows, d), dev)
+    pdb, lddb = _rows(db, "db", dt, (rows, d), dev)
+    param = lambda w: None if w is None else torch.empty(d, dtype=torch.float32, device=dev)  # noqa: E731
+    dw_post, dscale, dw_pre = param(w_post), param(scale), param(w_pre)
+    dgate = None if gate is None else torch.empty(gate.shape, dtype=dt, device=dev)
+    adr = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
+    lib = _lib()
+    size = _call(lib.janus_residual_norm_grad_workspace(C.byref(p)), "janus_residual_norm_grad_workspace")
+    with _on(dev) as stream:
+        work = torch.empty(size, dtype=torch.uint8, device=dev)
+        _call(lib.janus_residual_norm_grad(C.byref(p), pdr, lddr, pdn, lddn, pr, ldr, pb, ldb, pdx, lddx, pdb, lddb,
+                                           adr(dw_post), adr(dscale), adr(dw_pre), adr(dgate), d, work.data_ptr(), size,
+                                           stream), "janus_residual_norm_grad")
+    return NormGrads(dx, db, dw_post, dgate, dscale, dw_pre)
+
+
+def expert_layer(x, router, w_up, w_down, top_k, beta=None, normalize=False, out=None):
+    """A whole expert layer for up to 64 tokens x [tokens, d]: logits x router + beta, the top_k largest,
+    gates their softmax probabilities (normalize: divided by their sum), and
+    y = sum_c gate_c SiLU(x w_up[e_c]) w_down[e_c].
+
+    router [d, n] float32, beta [n] float32 or None, w_up [n, d, h] and w_down [n, h, d] of x's type; d and h
+    multiples of 16.  Returns (y [tokens, d], expert ids [tokens, top_k] int32, gates float32)."""
+    import torch
+    tokens, d, dev = _matrix(x, "x")
+    if not isinstance(w_up, torch.Tensor) or w_up.dim() != 3:
+        raise ValueError("w_up: expected a tensor [experts, d, hidden]")
+    n, _, h = w_up.shape
+    code = _type_of(x, "x")
+    px, ldx = _rows(x, "x", x.dtype, (tokens, d), dev)
+    _arg(router, "router", "f32", (d, n), dev)
+    for name, t, shape in (("w_up", w_up, (n, d, h)), ("w_down", w_down, (n, h, d))):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+        if t.dtype != x.dtype:
+            raise TypeError(f"{name}: dtype {t.dtype}, expected {x.dtype}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+        if t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name}: must be a contiguous tensor on {dev}")
+    p = Experts(d, h, n, int(top_k), code, int(bool(normalize)), router.data_ptr(), _param(beta, "beta", n, dev),
+                w_up.data_ptr(), w_down.data_ptr())
+    lib = _lib()
+    size = _call(lib.janus_expert_layer_workspace(C.byref(p), tokens), "janus_expert_layer_workspace")
+    y = torch.empty(tokens, d, dtype=x.dtype, device=dev) if out is None else out
+    py, ldy = _rows(y, "out", x.dtype, (tokens, d), dev)
+    eid = torch.empty(tokens, p.top_k, dtype=torch.int32, device=dev)
+    gate = torch.empty(tokens, p.top_k, dtype=torch.float32, device=dev)
+    with _on(dev) as stream:
+        work = torch.empty(size, dtype=torch.uint8, device=dev)
+        _call(lib.janus_expert_layer(C.byref(p), px, ldx, tokens, py, ldy, eid.data_ptr(), gate.data_ptr(),
+                                     work.data_ptr(), size, stream), "janus_expert_layer")
+    return y, eid, gate
+
+
+class PackedRows(NamedTuple):
+    """Activations in 8 bits: values q [rows, d] int8 and one code per 32 columns, code
+    [rows, ceil(d / 32)] uint8; a value stands for q 2^(code - 127), code 255 for NaN."""
+    q: object
+    code: object
+
+
+def _packed(p, device=None):
+    import torch
+    rows, d, dev = _matrix(p.q, "q")
+    if device is not None and dev != device:
+        raise ValueError(f"q: on {dev}, expected {device}")
+    pq, ldq = _rows(p.q, "q", torch.int8, (rows, d), dev)
+    pc, ldc = _rows(p.code, "code", torch.uint8, (rows, (d + 31) // 32), dev)
+    return rows, d, dev, (pq, ldq, pc, ldc)
+
+
+def pack_rows(x, out=None) -> PackedRows:
+    """x [rows, d] (float32, bfloat16 or float16) in 8 bits.  The values' rows start on multiples of 16 bytes;
+    out = PackedRows to write into."""
+    import torch
+    rows, d, dev = _matrix(x, "x")
+    code = _type_of(x, "x")
+    px, ldx = _rows(x, "x", x.dtype, (rows, d), dev)
+    if out is None:
+        out = PackedRows(torch.empty(rows, (d + 15) // 16 * 16, dtype=torch.int8, device=dev)[:, :d],
+                         torch.empty(rows, (d + 31) // 32, dtype=torch.uint8, device=dev))
+    n, w, _, at = _packed(out, dev)
+    if (n, w) != (rows, d):
+        raise ValueError(f"out: {n} x {w}, expected {rows} x {d}")
+    with _on(dev) as stream:
+        _call(_lib().janus_pack_rows(px, ldx, code, rows, d, *at, stream), "janus_pack_rows")
+    return out
+
+
+def unpack_rows(packed, dtype, act="none", grad=None, value=None, out=None):
+    """What packed rows stand for, as `dtype`.
+
+    act "none": returns X.  act "silu": returns SiLU(X), or with grad [rows, d] the gradient
+    grad * SiLU'(X), or with grad and value=True both as (gradient, SiLU(X)).  `out`: tensor for the
+    first result (it may be grad)."""
+    import torch
+    rows, d, dev, at = _packed(packed)
+    code = _type_of(dtype, "dtype")
+    if act not in ACT:
+        raise ValueError(f"act: {act!r}, expected one of {sorted(ACT)}")
+    if grad is not None and act == "none":
+        raise ValueError("grad: without an activation")
+    pg, ldg = (None, 0) if grad is None else _rows(grad, "grad", dtype, (rows, d), dev)
+    first = torch.empty(rows, d, dtype=dtype, device=dev) if out is None else out
+    pf, ldf = _rows(first, "out", dtype, (rows, d), dev)
+    second = torch.empty(rows, d, dtype=dtype, device=dev) if grad is not None and value else None
+    ps, lds = (None, 0) if second is None else _rows(second, "value", dtype, (rows, d), dev)
+    if grad is None:
+        ps, lds, pf, ldf = pf, ldf, None, 0
+    with _on(dev) as stream:
+        _call(_lib().janus_unpack_rows(*at, rows, d, code, ACT[act], pg, ldg, pf, ldf, ps, lds, stream),
+              "janus_unpack_rows")
+    return first if second is None else (first, second)
+
+
+def packed_wgrad(packed, B, row_off, out=None):
+    """Grouped weight gradient from activations in 8 bits: G_g = X_g^T B_g over the rows
+    row_off[g] .. row_off[g + 1] - 1 of X (packed [rows, P]) and B [rows, Q] (float32, bfloat16 or
+    float16); returns G [groups, P, Q] float32.  row_off [groups + 1] int32 on the device."""
+    import torch
+    rows, P, dev, at = _packed(packed)
+    n, Q, _ = _matrix(B, "B")
+    code = _type_of(B, "B")
+    pb, ldb = _rows(B, "B", B.dtype, (rows, Q), dev)
+    _arg(row_off, "row_off", "i32", (None,), dev)
+    G = row_off.shape[0] - 1
+    if out is None:
+        out = torch.empty(max(G, 0), P, Q, dtype=torch.float32, device=dev)
+    _arg(out, "out", "f32", (G, P, Q), dev)
+    lib = _lib()
+    size = _call(lib.janus_packed_wgrad_workspace(rows, G, P, Q, code), "janus_packed_wgrad_workspace")
+    with _on(dev) as stream:
+        work = torch.empty(size, dtype=torch.uint8, device=dev)
+        _call(lib.janus_packed_wgrad(*at, pb, ldb, code, out.data_ptr(), row_off.data_ptr(), G, rows, P, Q,
+                                     work.data_ptr(), size, stream), "janus_packed_wgrad")
     return out
 
 
