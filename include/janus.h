@@ -643,7 +643,7 @@ int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t
  *   G_g[p, c] = sum over the rows m of group g of X[m, p] B[m, c]
  * with X packed [rows, P], B [rows, Q] of `type`, G [n_groups, P, Q] fp32 and row_off [n_groups + 1]
  * int32 on the device, non-decreasing from 0 (row_off[n_groups] <= rows: rows behind the last group are not
- * read).  1..1024 groups; groups without rows get zeros.  Every product is exact in fp32, sums are held in
+ * read).  1..1024 groups, rows at most 2^31 - 4097; groups without rows get zeros.  Every product is exact in fp32, sums are held in
  * fp32 and split over row chunks that are added in a fixed order.  Offsets that break these rules
  * give wrong values but no access outside the arrays.
  */

@@ -19,81 +19,107 @@ struct ExpertArgs {
   const float* beta;
 };
 
-// Router of one token per workgroup: logits summed by 256 / 2^ceil(log2 n) threads per expert, then the
-// choice by one wave that holds four experts per lane.
-template <typename T>
-__global__ __launch_bounds__(256) void expert_route_kernel(ExpertArgs a, const T* __restrict__ x, long long ldx,
-                                                           int* __restrict__ eid, float* __restrict__ gate,
-                                                           int* __restrict__ arrived, int n_arrived) {
-  __shared__ float red[256], logit[kMaxExperts];
-  const int t = blockIdx.x;
-  if (t == 0)   // the counts of the second product's workgroups
-    for (int i = threadIdx.x; i < n_arrived; i += 256) arrived[i] = 0;
+// Router of one token by a workgroup of W waves.  Lanes take V neighbouring experts each (four where rows of the
+// router start on 16 bytes), the rest of a wave and the waves take rows, eight in flight; rows are added over
+// the lanes and then over the waves.  Every expert then counts those that come before it: its rank is its
+// place among the chosen, without a round for each of them.
+// NaN ranks like -inf and makes the token's gates NaN; a token without any finite or +inf logit
+// (all experts masked) has gates of zero.
+template <int W>
+struct RouteArea {
+  float red[W][kMaxExperts];
+  __align__(16) float key[kMaxExperts];
+  float sum[4], top[kMaxTopK], gate[kMaxTopK];
+  int eid[kMaxTopK], nan;
+};
+template <typename T, int V, int W>
+__device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __restrict__ x, RouteArea<W>& s) {
+  typedef float vec __attribute__((ext_vector_type(V)));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kFlight = 8;
+  const int units = (a.n + V - 1) / V;
   int wide = 1;
-  while (wide < a.n) wide <<= 1;
-  const int e = threadIdx.x & (wide - 1), part = threadIdx.x / wide, parts = 256 / wide;
-  float s = 0.f;
-  if (e < a.n)
-    for (int i = part; i < a.d; i += parts) s += (float)x[t * ldx + i] * a.router[(long long)i * a.n + e];
-  red[threadIdx.x] = s;
-  __syncthreads();
-  if ((int)threadIdx.x < a.n) {
-    float v = 0.f;
-    for (int p = 0; p < parts; ++p) v += red[p * wide + threadIdx.x];
-    logit[threadIdx.x] = v + (a.beta ? a.beta[threadIdx.x] : 0.f);
-  }
-  __syncthreads();
-  if (threadIdx.x >= 64) return;
-  // NaN ranks like -inf and makes the token's gates NaN; a token without any finite or +inf logit
-  // (all experts masked) has gates of zero
-  float l[4], key[4], top = -INFINITY;
-  bool taken[4];
+  while (wide < units && wide < 64) wide <<= 1;
+  const int per = 64 / wide, rows = per * W, row0 = wave * per + lane / wide;
+  if (threadIdx.x == 0) s.nan = 0;
+  for (int u0 = 0; u0 < units; u0 += 64) {
+    const int u = u0 + (lane & (wide - 1));
+    vec sum = {};
+    const float* w = a.router + V * min(u, units - 1);
+    for (int i = row0; i < a.d; i += kFlight * rows) {
+      vec r[kFlight];
+      float v[kFlight];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int q = threadIdx.x + 64 * j;
-    l[j] = q < a.n ? logit[q] : -INFINITY;
-    taken[j] = q >= a.n;
-    key[j] = l[j] == l[j] ? l[j] : -INFINITY;
-    top = fmaxf(top, key[j]);
-  }
-  bool nan = false;
+      for (int j = 0; j < kFlight; ++j) {
+        const int q = min(i + j * rows, a.d - 1);
+        r[j] = *reinterpret_cast<const vec*>(w + (long long)q * a.n);
+        v[j] = (float)x[q];
+      }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) nan |= l[j] != l[j];
-  nan = __any(nan);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  float p[4], sum = 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    p[j] = top == -INFINITY ? 0.f : expf(l[j] - top);
-    if ((int)threadIdx.x + 64 * j >= a.n) p[j] = 0.f;
-    sum += p[j];
-  }
-  sum = wave_sum(sum);
-  float chosen = 0.f, mine = 0.f;
-  int mine_e = 0;
-  for (int c = 0; c < a.k; ++c) {
-    float best = -INFINITY, bp = 0.f;
-    int at = INT_MAX;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (!taken[j] && (at == INT_MAX || key[j] > best)) best = key[j], bp = p[j], at = threadIdx.x + 64 * j;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float v = __shfl_xor(best, o, 64), vp = __shfl_xor(bp, o, 64);
-      const int va = __shfl_xor(at, o, 64);
-      if (va != INT_MAX && (at == INT_MAX || v > best || (v == best && va < at))) best = v, bp = vp, at = va;
+      for (int j = 0; j < kFlight; ++j)
+        if (i + j * rows < a.d) sum += r[j] * v[j];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if ((int)threadIdx.x + 64 * j == at) taken[j] = true;
-    chosen += bp;
-    if ((int)threadIdx.x == c) mine = bp, mine_e = at;
+    for (int c = 0; c < V; ++c) {
+      for (int o = wide; o < 64; o <<= 1) sum[c] += __shfl_xor(sum[c], o, 64);
+      if (lane < wide && u < units) s.red[wave][V * u + c] = sum[c];
+    }
   }
-  const float over = a.normalize ? chosen : sum;
+  __syncthreads();
+  const int e = threadIdx.x;
+  float l = -INFINITY, key = -INFINITY;
+  if (e < a.n) {
+    l = 0.f;
+#pragma unroll
+    for (int p = 0; p < W; ++p) l += s.red[p][e];
+    if (a.beta) l += a.beta[e];
+    if (l == l) key = l;
+    else s.nan = 1;
+  }
+  if (e < kMaxExperts) s.key[e] = key;
+  __syncthreads();
+  int rank = 0;
+  if (e < a.n) {
+    for (int q = 0; q < a.n; q += 4) {   // keys past the last expert are -inf and of a higher index
+      const f32x4 o = *reinterpret_cast<const f32x4*>(s.key + q);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rank += o[j] > key || (o[j] == key && q + j < e);
+    }
+    if (rank < a.k) s.top[rank] = key, s.eid[rank] = e;
+  }
+  __syncthreads();
+  const float top = s.top[0];
+  if (e < kMaxExperts) {
+    const float p = wave_sum(top == -INFINITY ? 0.f : expf(l - top));
+    if (lane == 0) s.sum[wave] = p;
+  }
+  __syncthreads();
+  if (e < a.k) {
+    auto p = [&](int c) { return top == -INFINITY ? 0.f : expf(s.top[c] - top); };
+    float over = 0.f;
+    if (a.normalize)
+      for (int c = 0; c < a.k; ++c) over += p(c);
+    else
+      over = (s.sum[0] + s.sum[1]) + (s.sum[2] + s.sum[3]);
+    s.gate[e] = s.nan ? NAN : over > 0.f || over != over ? p(e) / over : 0.f;
+  }
+  __syncthreads();
+}
+
+constexpr int kRouteWaves = 16;
+template <typename T, int V>
+__global__ __launch_bounds__(64 * kRouteWaves) void expert_route_kernel(ExpertArgs a, const T* __restrict__ x,
+                                                                        long long ldx, int* __restrict__ eid,
+                                                                        float* __restrict__ gate,
+                                                                        int* __restrict__ arrived, int n_arrived) {
+  __shared__ RouteArea<kRouteWaves> s;
+  const int t = blockIdx.x;
+  if (t == 0)   // the counts of the second product's workgroups
+    for (int i = threadIdx.x; i < n_arrived; i += 64 * kRouteWaves) arrived[i] = 0;
+  route_token<T, V, kRouteWaves>(a, x + t * ldx, s);
   if ((int)threadIdx.x < a.k) {
-    eid[t * a.k + threadIdx.x] = mine_e;
-    gate[t * a.k + threadIdx.x] = nan ? NAN : over > 0.f || over != over ? mine / over : 0.f;
+    eid[t * a.k + threadIdx.x] = s.eid[threadIdx.x];
+    gate[t * a.k + threadIdx.x] = s.gate[threadIdx.x];
   }
 }
 
@@ -308,23 +334,62 @@ __device__ __forceinline__ void expert_product(const ExpertSlots& s, const S* __
 }
 
 // hidden[slot, j] = SiLU(sum_i x[i] W1[e, i, j])
-template <typename T, int COLS, int MT>
+// kRoute (one token): every workgroup routes the token itself, with V experts per lane, and the first one
+// writes the choice.
+template <typename T, int COLS, int MT, int V, bool kRoute>
 __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs a, const T* __restrict__ x,
                                                                       long long ldx, const T* __restrict__ w1,
-                                                                      const int* __restrict__ eid,
+                                                                      int* __restrict__ eid, float* __restrict__ gate,
+                                                                      int* __restrict__ arrived, int n_arrived,
                                                                       float* __restrict__ hidden) {
   __shared__ ExpertSlots s;
   __shared__ float lds[kExpertWaves * 256 * COLS];
-  if (find_slots(a, eid, s) == 0) return;
+  if constexpr (kRoute) {
+    __shared__ RouteArea<kExpertWaves> r;
+    route_token<T, V, kExpertWaves>(a, x, r);
+    if (blockIdx.x == 0 && blockIdx.y == 0) {
+      for (int i = threadIdx.x; i < n_arrived; i += 64 * kExpertWaves) arrived[i] = 0;
+      if ((int)threadIdx.x < a.k) eid[threadIdx.x] = r.eid[threadIdx.x], gate[threadIdx.x] = r.gate[threadIdx.x];
+    }
+    if (threadIdx.x == 0) s.count = 1, s.slot[0] = blockIdx.y, s.expert = r.eid[blockIdx.y];
+    __syncthreads();
+  } else {
+    if (find_slots(a, eid, s) == 0) return;
+  }
   expert_product<T, T, Eight<T>, COLS, MT>(s, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d, a.d, lds,
                                            [&](int t, int c, float v) {
                                              hidden[(long long)s.slot[t] * a.h + c] = silu(v);
                                            });
 }
 
-// part[slot, split, i] = sum over the split's rows j of hidden[slot, j] W2[e, j, i]; the last workgroup of a
-// column block to finish adds the parts of every token: y = sum_c gate sum_split part, in that order.
-template <typename T, int COLS, int MT>
+// y[t, c] = sum_q gate[t, q] sum_z part[t k + q, z, c] in that order, eight parts in flight.
+template <typename F>
+__device__ __forceinline__ float expert_sum(const ExpertArgs& a, const float* __restrict__ gate, float* part, int splits,
+                                            int t, int c, F load) {
+  const int n = a.k * splits;
+  const float* g = gate + t * a.k;
+  float* p = part + (long long)t * n * a.d + c;
+  float out = 0.f, v = 0.f;
+  for (int i = 0; i < n; i += 8) {
+    float u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = load(p + (long long)min(i + j, n - 1) * a.d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j < n) {
+        v += u[j];
+        if ((i + j + 1) % splits == 0) out += g[(i + j) / splits] * v, v = 0.f;
+      }
+  }
+  return out;
+}
+
+// part[slot, split, i] = sum over the split's rows j of hidden[slot, j] W2[e, j, i].
+// kJoin: the last workgroup of a column block to finish adds the parts (expert_sum); else expert_join_kernel does.
+// The parts then cross the dies' L2 caches, so they are written and read as relaxed atomics of device scope,
+// which pass those caches by; a wave waits for its own to be done before the workgroup's arrival is counted.
+// (A device-scope fence in their place writes back a whole L2 per wave: 36 against 11 us for one token.)
+template <typename T, int COLS, int MT, bool kJoin>
 __global__ __launch_bounds__(64 * kExpertWaves) void expert_down_kernel(ExpertArgs a, const float* __restrict__ hidden,
                                                                         const T* __restrict__ w2,
                                                                         const int* __restrict__ eid,
@@ -339,34 +404,46 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_down_kernel(ExpertAr
   if (find_slots(a, eid, s) > 0)
     expert_product<T, float, A, COLS, MT>(s, hidden, a.h, 1, w2 + (long long)s.expert * a.h * a.d, a.d, k0,
                                           min(k0 + rows_per_split, a.h), a.h, lds, [&](int t, int c, float v) {
-                                            part[((long long)s.slot[t] * splits + blockIdx.z) * a.d + c] = v;
+                                            float* o = part + ((long long)s.slot[t] * splits + blockIdx.z) * a.d + c;
+                                            if constexpr (kJoin)
+                                              __hip_atomic_store(o, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                                            else
+                                              *o = v;
                                           });
-  __threadfence();   // this thread's parts before the workgroup's arrival
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(arrived + blockIdx.x, 1) == (int)(gridDim.y * gridDim.z) - 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();   // the others' parts after their arrival
-  const int c0 = blockIdx.x * (16 * COLS);
-  for (int e = threadIdx.x; e < a.tokens * 16 * COLS; e += 64 * kExpertWaves) {
-    const int t = e / (16 * COLS), c = c0 + e % (16 * COLS);
-    if (c >= a.d) continue;
-    float out = 0.f;
-    for (int q = 0; q < a.k; ++q) {
-      const float* p = part + (long long)(t * a.k + q) * splits * a.d + c;
-      float v = 0.f;
-      for (int z = 0; z < splits; ++z) v += p[(long long)z * a.d];
-      out += gate[t * a.k + q] * v;
+  if constexpr (kJoin) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(arrived + blockIdx.x, 1) == (int)(gridDim.y * gridDim.z) - 1;
+    __syncthreads();
+    if (!last) return;
+    const int c0 = blockIdx.x * (16 * COLS);
+    for (int e = threadIdx.x; e < a.tokens * 16 * COLS; e += 64 * kExpertWaves) {
+      const int t = e / (16 * COLS), c = c0 + e % (16 * COLS);
+      if (c < a.d)
+        y[t * ldy + c] = (T)expert_sum(a, gate, part, splits, t, c, [](float* p) {
+          return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        });
     }
-    y[t * ldy + c] = (T)out;
   }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void expert_join_kernel(ExpertArgs a, const float* __restrict__ gate, float* part,
+                                                          int splits, T* __restrict__ y, long long ldy) {
+  const int c = blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
+  if (c < a.d) y[t * ldy + c] = (T)expert_sum(a, gate, part, splits, t, c, [](float* p) { return *p; });
 }
 
 // How a call is shared out.  A workgroup takes one expert and 64 (16-bit types: 128) columns; where that leaves
 // fewer than 256 workgroups, half as many columns.  The second product is also cut along its
-// rows, into at most one stage of 32 rows per wave, until there are 512 workgroups.
+// rows, into at most one stage of 32 rows per wave, until there are 512 workgroups.  Its parts are joined by the last
+// workgroup of each column block where that has one value per thread or less, else (a few workgroups would
+// join for long while the others idle) by a kernel of their own.  One token is routed by every workgroup of the
+// first product where the router is small (up to 256 KB, read from L2 in little more than the time of the
+// launch that this saves).
 struct ExpertPlan {
   int experts, cols_up, cols_down, splits, rows_per_split;
+  bool join, route_inside;
 };
 static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
   ExpertPlan q;
@@ -381,6 +458,8 @@ static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
   q.splits = want < most ? want : most;
   q.rows_per_split = (int)cdiv(cdiv(p->d_hidden, q.splits), 32) * 32;
   q.splits = (int)cdiv(p->d_hidden, q.rows_per_split);
+  q.join = tokens * 16 * q.cols_down <= 64 * kExpertWaves;
+  q.route_inside = tokens == 1 && (long long)p->d * p->n_experts <= 65536;
   return q;
 }
 struct ExpertWork {
@@ -439,29 +518,52 @@ extern "C" int janus_expert_layer(const janus_experts* p, const void* x, int64_t
   int* arrived = reinterpret_cast<int*>(base + at.arrived);
   with_type(p->type, [&](auto zero) {
     using T = decltype(zero);
-    hipLaunchKernelGGL(expert_route_kernel<T>, dim3(tokens), dim3(256), 0, st, a, static_cast<const T*>(x), ldx, eid,
-                       gate, arrived, (int)cdiv(a.d, 16 * plan.cols_down));
-    auto product = [&](auto cols, auto mt, bool up) {
-      constexpr int kCols = decltype(cols)::value, kTiles = decltype(mt)::value;
-      const unsigned bx = cdiv(up ? a.h : a.d, 16 * kCols);
-      if (up)
-        hipLaunchKernelGGL((expert_up_kernel<T, kCols, kTiles>), dim3(bx, plan.experts), dim3(64 * kExpertWaves), 0, st,
-                           a, static_cast<const T*>(x), ldx, static_cast<const T*>(p->w_up), eid, hidden);
-      else
-        hipLaunchKernelGGL((expert_down_kernel<T, kCols, kTiles>), dim3(bx, plan.experts, plan.splits),
-                           dim3(64 * kExpertWaves), 0, st, a, hidden, static_cast<const T*>(p->w_down), eid, gate, part,
-                           arrived, plan.rows_per_split, static_cast<T*>(y), ldy);
+    const int counts = (int)cdiv(a.d, 16 * plan.cols_down);
+    const T* xt = static_cast<const T*>(x);
+    const T* up = static_cast<const T*>(p->w_up);
+    auto by_columns = [&](int cols, auto f) {
+      constexpr int kWide = sizeof(T) == 4 ? 4 : 8;
+      if (cols == kWide) f(std::integral_constant<int, kWide>{});
+      else f(std::integral_constant<int, kWide / 2>{});
     };
-    auto with_tiles = [&](auto cols, bool up) {
-      if (tokens <= 16) product(cols, std::integral_constant<int, 1>{}, up);
-      else if (tokens <= 32) product(cols, std::integral_constant<int, 2>{}, up);
-      else product(cols, std::integral_constant<int, 4>{}, up);
+    auto by_tiles = [&](auto f) {
+      if (tokens <= 16) f(std::integral_constant<int, 1>{});
+      else if (tokens <= 32) f(std::integral_constant<int, 2>{});
+      else f(std::integral_constant<int, 4>{});
     };
-    constexpr int kWide = sizeof(T) == 4 ? 4 : 8;
-    for (const bool up : {true, false}) {
-      if ((up ? plan.cols_up : plan.cols_down) == kWide) with_tiles(std::integral_constant<int, kWide>{}, up);
-      else with_tiles(std::integral_constant<int, kWide / 2>{}, up);
+    auto by_router = [&](auto f) {
+      if (a.n % 4 == 0 && rows_aligned(a.router, 0, 4)) f(std::integral_constant<int, 4>{});
+      else f(std::integral_constant<int, 1>{});
+    };
+    auto launch_up = [&](auto cols, auto mt, auto v, auto routes) {
+      hipLaunchKernelGGL((expert_up_kernel<T, cols.value, mt.value, v.value, routes.value>),
+                         dim3(cdiv(a.h, 16 * cols.value), plan.experts), dim3(64 * kExpertWaves), 0, st, a, xt, ldx, up,
+                         eid, gate, arrived, counts, hidden);
+    };
+    auto launch_down = [&](auto cols, auto mt, auto join) {
+      hipLaunchKernelGGL((expert_down_kernel<T, cols.value, mt.value, join.value>),
+                         dim3(cdiv(a.d, 16 * cols.value), plan.experts, plan.splits), dim3(64 * kExpertWaves), 0, st, a,
+                         hidden, static_cast<const T*>(p->w_down), eid, gate, part, arrived, plan.rows_per_split,
+                         static_cast<T*>(y), ldy);
+    };
+    const std::integral_constant<int, 1> one;
+    if (plan.route_inside) {
+      by_columns(plan.cols_up, [&](auto cols) { by_router([&](auto v) { launch_up(cols, one, v, std::true_type{}); }); });
+    } else {
+      by_router([&](auto v) {
+        hipLaunchKernelGGL((expert_route_kernel<T, v.value>), dim3(tokens), dim3(64 * kRouteWaves), 0, st, a, xt, ldx,
+                           eid, gate, arrived, counts);
+      });
+      by_columns(plan.cols_up,
+                 [&](auto cols) { by_tiles([&](auto mt) { launch_up(cols, mt, one, std::false_type{}); }); });
     }
+    by_columns(plan.cols_down, [&](auto cols) {
+      if (plan.join) launch_down(cols, one, std::true_type{});
+      else by_tiles([&](auto mt) { launch_down(cols, mt, std::false_type{}); });
+    });
+    if (!plan.join)
+      hipLaunchKernelGGL(expert_join_kernel<T>, dim3(cdiv(a.d, 256), tokens), dim3(256), 0, st, a, gate, part,
+                         plan.splits, static_cast<T*>(y), ldy);
   });
   return launched();
 }

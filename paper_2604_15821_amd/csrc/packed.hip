@@ -131,39 +131,333 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
   }
 }
 
-// G_g[p, q] = sum over the rows m of group g of X[m, p] B[m, q]: 64 x 64 tiles, 16 rows at a time.
+// ------------------------------------------------------------------ the weight gradient
+// G_g[p, c] = sum over the rows m of group g of X[m, p] B[m, c] on the bf16 matrix instructions
+// (v_mfma_f32_32x32x16_bf16).  X is exact in bf16; B is taken as it is (bf16), as two bf16 terms (fp16: eight and three of its
+// eleven bits) or three (fp32: eight bits each, by truncation), which sum to it exactly, so every product is exact.
+//
+// A workgroup of four waves (2 x 2) owns 128 rows p and COLS columns of a group's chunk of rows m (COLS = 256
+// with one term, else 128).  Both operands arrive with p and c, not m, along memory rows.  They are put into LDS as they
+// come, [32 m][p or c] in bf16, and read with the transposing ds_read_b64_tr_b16: 16 lanes give the addresses of
+// four rows of 16 values and receive four m of one column each, two reads an operand of the 32 x 32 x 16
+// instruction.  The 32-byte units of a row are stored at unit ^ (m % 8), so that the four rows of a read fall on
+// different banks.  Stages of 32 rows alternate between two LDS buffers, and the registers of a stage are
+// loaded two stages before it is multiplied.
+//
+// Rows are cut into chunks, a group's longest first and given to the dies in turn, so that the tiles of a chunk
+// share its die's L2 and none runs long at the end.  A group's only chunk writes the gradient itself; else
+// each writes a partial and a second kernel adds them in order.
+struct PackedChunk {
+  int group, r0, r1, alone;
+};
+
+constexpr int kWgP = 128, kWgRows = 32;
+
 template <typename T>
-__global__ __launch_bounds__(256) void packed_wgrad_kernel(const int8_t* __restrict__ q, long long ldq,
-                                                           const uint8_t* __restrict__ code, long long ldc,
-                                                           const T* __restrict__ b, long long ldb, int P, int Q,
-                                                           const int* __restrict__ off, long long rows,
-                                                           float* __restrict__ G) {
-  __shared__ float A[16][64], B[16][64];
-  const int p0 = blockIdx.x * 64, q0 = blockIdx.y * 64, g = blockIdx.z;
-  const long long m0 = max(off[g], 0), m1 = min((long long)off[g + 1], rows);
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  float acc[4][4] = {};
-  for (long long m = m0; m < m1; m += 16) {
-    for (int e = threadIdx.x; e < 1024; e += 256) {
-      const int r = e >> 6, c = e & 63;
-      const long long row = m + r;
-      A[r][c] = row < m1 && p0 + c < P
-                    ? (float)q[row * ldq + p0 + c] * code_scale(code[row * ldc + (p0 + c) / kPackBlock]) : 0.f;
-      B[r][c] = row < m1 && q0 + c < Q ? (float)b[row * ldb + q0 + c] : 0.f;
+struct Terms;
+template <>
+struct Terms<__bf16> {
+  static constexpr int kPlanes = 1, kCols = 256;
+};
+template <>
+struct Terms<_Float16> {
+  static constexpr int kPlanes = 2, kCols = 128;
+};
+template <>
+struct Terms<float> {
+  static constexpr int kPlanes = 3, kCols = 128;
+};
+
+__device__ __forceinline__ unsigned pack_high(float a, float b) {   // the upper halves, a first
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
+
+// Eight values of a row of B, and their planes.
+template <typename T>
+struct Octet {
+  T v[8];
+  template <bool WIDE>
+  __device__ __forceinline__ void load(const T* __restrict__ row, int c, int n) {
+    if constexpr (WIDE) {
+      typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+      constexpr int V = 16 / (int)sizeof(T);
+#pragma unroll
+      for (int j = 0; j < 8; j += V) {   // a run that begins past the row reads the first one, and is not stored
+        const vec u = *reinterpret_cast<const vec*>(row + (c + j < n ? c + j : 0));
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j + i] = u[i];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = row[min(c + j, n - 1)];
     }
-    __syncthreads();
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += A[r][ty * 4 + i] * B[r][tx * 4 + j];
-    __syncthreads();
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int p = p0 + ty * 4 + i, c = q0 + tx * 4 + j;
-      if (p < P && c < Q) G[((long long)g * P + p) * Q + c] = acc[i][j];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (T)0.f;
+  }
+  __device__ __forceinline__ void planes(uint4 (&o)[Terms<T>::kPlanes]) const {
+    if constexpr (Terms<T>::kPlanes == 1) {
+      __builtin_memcpy(&o[0], v, 16);
+    } else {
+      unsigned w[Terms<T>::kPlanes][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a = (float)v[2 * i], b = (float)v[2 * i + 1];
+#pragma unroll
+        for (int q = 0; q < Terms<T>::kPlanes; ++q) {
+          w[q][i] = pack_high(a, b);
+          a -= high_part(a);
+          b -= high_part(b);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < Terms<T>::kPlanes; ++q) o[q] = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
     }
+  }
+};
+
+// Sixteen packed values of a row and their scale, as bf16.
+struct Sixteen {
+  uint4 q;
+  int code;
+  template <bool WIDE>
+  __device__ __forceinline__ void load(const int8_t* __restrict__ row, const uint8_t* __restrict__ codes, int c, int n) {
+    if constexpr (WIDE) {
+      q = *reinterpret_cast<const uint4*>(row + (c < n ? c : 0));
+    } else {
+      unsigned w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w[j >> 2] |= (unsigned)(uint8_t)row[min(c + j, n - 1)] << (8 * (j & 3));
+      q = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    code = codes[min(c, n - 1) / kPackBlock];
+  }
+  __device__ __forceinline__ void clear() { code = 0; }   // a scale of zero
+  __device__ __forceinline__ void values(uint4 (&o)[2]) const {
+    const float s = code_scale(code);
+    const unsigned in[4] = {q.x, q.y, q.z, q.w};
+    unsigned w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned u = in[i >> 1] >> (16 * (i & 1));
+      w[i] = pack_high((float)(int8_t)u * s, (float)(int8_t)(u >> 8) * s);
+    }
+    o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ bf16x8 read_columns(const char* lo, const char* hi) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __restrict__ q, long long ldq,
+                                                              const uint8_t* __restrict__ code, long long ldc,
+                                                              const T* __restrict__ b, long long ldb, int P, int Q,
+                                                              const PackedChunk* __restrict__ chunks,
+                                                              const int* __restrict__ n_chunks, int tiles_p,
+                                                              int tiles_q, float* __restrict__ partial,
+                                                              float* __restrict__ G) {
+  constexpr int NP = Terms<T>::kPlanes, COLS = Terms<T>::kCols;
+  constexpr int kPass = COLS / 64, kFrag = COLS / 64;   // octets of B per thread and stage; 32-column blocks per wave
+  constexpr int kRowA = kWgP * 2, kRowB = COLS * 2, kBytesA = kWgRows * kRowA, kBytesB = kWgRows * kRowB;
+  constexpr int kStage = kBytesA + NP * kBytesB;
+  __shared__ __align__(16) char lds[2 * kStage];
+  // block -> die block % 8 -> chunk, tile: the tiles of a chunk are consecutive blocks of one die
+  const int tiles = tiles_p * tiles_q, slot = blockIdx.x >> 3;
+  const int at = slot / tiles * 8 + (blockIdx.x & 7), tile = slot % tiles;
+  if (at >= *n_chunks) return;
+  const PackedChunk ch = chunks[at];
+  const int p0 = tile / tiles_q * kWgP, c0 = tile % tiles_q * COLS;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+
+  // staging: thread t holds 16 values of X's row t / 8 and, per pass, 8 values of a row of B
+  const int ma = t >> 3, ua = t & 7, colA = p0 + 16 * ua;
+  const int wa = ma * kRowA + ((ua ^ (ma & 7)) << 5);
+  constexpr int kPerRow = COLS / 8, kRowsPass = 256 / kPerRow;
+  const int mb = t / kPerRow, ob = t % kPerRow, colB = c0 + 8 * ob;
+  struct Regs {
+    Sixteen a;
+    Octet<T> b[kPass];
+  };
+  auto load = [&](Regs& r, int m0) {
+    const long long ra = min(m0 + ma, ch.r1 - 1);
+    r.a.template load<WIDE>(q + ra * ldq, code + ra * ldc, colA, P);
+#pragma unroll
+    for (int i = 0; i < kPass; ++i)
+      r.b[i].template load<WIDE>(b + (long long)min(m0 + mb + i * kRowsPass, ch.r1 - 1) * ldb, colB, Q);
+  };
+  auto stage = [&](Regs& r, int m0, char* to) {
+    if (m0 + kWgRows > ch.r1) {   // rows past the end count as zero
+      if (m0 + ma >= ch.r1) r.a.clear();
+#pragma unroll
+      for (int i = 0; i < kPass; ++i)
+        if (m0 + mb + i * kRowsPass >= ch.r1) r.b[i].clear();
+    }
+    uint4 o[2];
+    r.a.values(o);
+    *reinterpret_cast<uint4*>(to + wa) = o[0];
+    *reinterpret_cast<uint4*>(to + wa + 16) = o[1];
+#pragma unroll
+    for (int i = 0; i < kPass; ++i) {
+      const int m = mb + i * kRowsPass;
+      uint4 w[NP];
+      r.b[i].planes(w);
+      char* at_b = to + kBytesA + m * kRowB + (((ob >> 1) ^ (m & 7)) << 5) + ((ob & 1) << 4);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) *reinterpret_cast<uint4*>(at_b + n * kBytesB) = w[n];
+    }
+  };
+
+  // operand addresses: 16-lane group g reads columns 16 (g % 2) .. + 15 and rows 8 (g / 2) + 4 h + r
+  const int g = lane >> 4, r = (lane >> 2) & 3, sub = (lane & 3) * 8;
+  int fa[2][2], fb[kFrag][2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int m = 8 * (g >> 1) + 4 * h + r;
+#pragma unroll
+    for (int f = 0; f < 2; ++f) fa[f][h] = m * kRowA + ((((wave >> 1) * 4 + 2 * f + (g & 1)) ^ (m & 7)) << 5) + sub;
+#pragma unroll
+    for (int f = 0; f < kFrag; ++f)
+      fb[f][h] = kBytesA + m * kRowB + ((((wave & 1) * (COLS / 32) + 2 * f + (g & 1)) ^ (m & 7)) << 5) + sub;
+  }
+  f32x16 acc[2][kFrag];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < kFrag; ++j) acc[i][j] = f32x16{};
+  auto multiply = [&](const char* from) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      bf16x8 x[2];
+#pragma unroll
+      for (int f = 0; f < 2; ++f) x[f] = read_columns(from + fa[f][0] + kb * 16 * kRowA, from + fa[f][1] + kb * 16 * kRowA);
+#pragma unroll
+      for (int n = NP - 1; n >= 0; --n)   // small terms first
+#pragma unroll
+        for (int f = 0; f < kFrag; ++f) {
+          const int o = n * kBytesB + kb * 16 * kRowB;
+          const bf16x8 y = read_columns(from + fb[f][0] + o, from + fb[f][1] + o);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y, acc[i][f], 0, 0, 0);
+        }
+    }
+  };
+
+  Regs r0, r1;
+  const int steps = (ch.r1 - ch.r0 + kWgRows - 1) / kWgRows;
+  load(r0, ch.r0);
+  stage(r0, ch.r0, lds);
+  load(r0, ch.r0 + kWgRows);
+  __syncthreads();
+  auto step = [&](int s, Regs& next, Regs& after) {   // multiplies stage s; `next` holds stage s + 1
+    const int m = ch.r0 + s * kWgRows;
+    load(after, m + 2 * kWgRows);
+    multiply(lds + (s & 1) * kStage);
+    stage(next, m + kWgRows, lds + ((s + 1) & 1) * kStage);
+    __syncthreads();
+  };
+  for (int s = 0; s < steps; s += 2) {
+    step(s, r0, r1);
+    if (s + 1 < steps) step(s + 1, r1, r0);
+  }
+
+  float* out = ch.alone ? G + (long long)ch.group * P * Q : partial + (long long)at * P * Q;
+  // row 8 (k / 4) + 4 (lane / 32) + k % 4 of a block, column lane % 32
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int f = 0; f < kFrag; ++f) {
+      const int c = c0 + (wave & 1) * (COLS / 2) + 32 * f + (lane & 31);
+      const int p = p0 + (wave >> 1) * 64 + 32 * i + 4 * (lane >> 5);
+      if (c < Q) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const int row = p + 8 * (k >> 2) + (k & 3);
+          if (row < P) __builtin_nontemporal_store(acc[i][f][k], out + (long long)row * Q + c);
+        }
+      }
+    }
+}
+
+// Chunks of at most kc rows, equally long within a group, groups with the longest chunks first.  first[g]: a
+// group's first chunk, count[g]: how many.  Offsets are held to [0, rows], so chunks always lie inside.
+__global__ __launch_bounds__(1024) void packed_chunks_kernel(const int* __restrict__ off, int groups, long long rows,
+                                                             int kc, PackedChunk* __restrict__ chunks, int most,
+                                                             int* __restrict__ n_chunks, int* __restrict__ first,
+                                                             int* __restrict__ count) {
+  __shared__ int len[1024], n[1024];
+  const int g = threadIdx.x;
+  int a = 0, size = 0;
+  if (g < groups) {
+    a = min(max(off[g], 0), (int)rows);
+    size = max(min(max(off[g + 1], 0), (int)rows) - a, 0);
+  }
+  const int mine = (size + kc - 1) / kc;
+  const int each = mine ? ((size + mine - 1) / mine + kWgRows - 1) / kWgRows * kWgRows : 0;
+  n[g] = mine ? (size + each - 1) / each : 0;
+  len[g] = each;
+  __syncthreads();
+  int at = 0, all = 0;
+  for (int o = 0; o < groups; ++o) {
+    at += len[o] > len[g] || (len[o] == len[g] && o < g) ? n[o] : 0;
+    all += n[o];
+  }
+  if (g < groups) {
+    first[g] = at;
+    const int held = min(n[g], max(most - at, 0));   // fewer only where offsets overlap
+    count[g] = held;
+    for (int i = 0; i < held; ++i)
+      chunks[at + i] = PackedChunk{g, a + i * each, a + (int)min((i + 1ll) * each, (long long)size), n[g] == 1};
+  }
+  if (g == 0) *n_chunks = min(all, most);
+}
+
+// Adds the partials of groups with several chunks, in order, and clears groups with none.
+__global__ __launch_bounds__(256) void packed_reduce_kernel(const float* __restrict__ partial,
+                                                            const int* __restrict__ first,
+                                                            const int* __restrict__ count, long long PQ,
+                                                            float* __restrict__ G) {
+  const int g = blockIdx.y, n = count[g];
+  if (n == 1) return;
+  const float* p = partial + first[g] * PQ;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < PQ; i += (long long)gridDim.x * 256) {
+    float v = 0.f;
+    for (int k = 0; k < n; ++k) v += p[k * PQ + i];
+    G[g * PQ + i] = v;
+  }
+}
+
+struct WgradPlan {
+  int tiles_p, tiles_q, kc, most;
+  int64_t chunks, first, count, partial, total;   // offsets in bytes
+};
+// The chunk length: half of what each of 512 resident workgroups would get of all stages, so that the last ones end
+// together; not below 256 rows, where partials cost more than they save.
+static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
+  WgradPlan w;
+  w.tiles_p = (int)cdiv(P, kWgP);
+  w.tiles_q = (int)cdiv(Q, type == JANUS_BF16 ? Terms<__bf16>::kCols : Terms<float>::kCols);
+  const double share = (double)rows * w.tiles_p * w.tiles_q / 1024;
+  const double kc = share < 256 ? 256 : share > 1e9 ? 1e9 : share;
+  w.kc = (int)((kc + kWgRows - 1) / kWgRows) * kWgRows;
+  w.most = (int)(groups + rows / w.kc);
+  w.chunks = 16;
+  w.first = w.chunks + (int64_t)w.most * sizeof(PackedChunk);
+  w.count = w.first + 4 * (int64_t)groups;
+  w.partial = (w.count + 4 * (int64_t)groups + 15) / 16 * 16;
+  w.total = w.partial + 4 * (int64_t)w.most * P * Q;
+  return w;
 }
 
 static PackShape pack_shape(long long rows, int d) {
@@ -233,7 +527,7 @@ extern "C" int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* co
 }
 
 static int check_packed_wgrad(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type) {
-  if (rows < 0 || rows > INT_MAX || n_groups < 1 || n_groups > 1024 || P < 1 || Q < 1 || !type_known(type))
+  if (rows < 0 || rows > INT_MAX - 4096 || n_groups < 1 || n_groups > 1024 || P < 1 || Q < 1 || !type_known(type))
     return JANUS_EINVAL;
   return JANUS_OK;
 }
@@ -241,7 +535,7 @@ static int check_packed_wgrad(int64_t rows, int32_t n_groups, int32_t P, int32_t
 extern "C" int64_t janus_packed_wgrad_workspace(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type) {
   int rc = check_packed_wgrad(rows, n_groups, P, Q, type);
   if (rc) return rc;
-  return 16;
+  return wgrad_plan(rows, n_groups, P, Q, type).total;
 }
 
 extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t ldc, const void* B,
@@ -253,11 +547,31 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
   if (!G || !row_off || (rows > 0 && (!B || ldb < Q)) || !work || !rows_aligned(work, 0, 1) ||
       work_bytes < janus_packed_wgrad_workspace(rows, n_groups, P, Q, type))
     return JANUS_EINVAL;
+  const WgradPlan w = wgrad_plan(rows, n_groups, P, Q, type);
+  const int64_t blocks = ((int64_t)w.most + 7) / 8 * 8 * w.tiles_p * w.tiles_q;
+  if (blocks > INT_MAX) return JANUS_EUNSUPPORTED;
+  char* base = static_cast<char*>(work);
+  int* n_chunks = reinterpret_cast<int*>(base);
+  PackedChunk* chunks = reinterpret_cast<PackedChunk*>(base + w.chunks);
+  int* first = reinterpret_cast<int*>(base + w.first);
+  int* count = reinterpret_cast<int*>(base + w.count);
+  float* partial = reinterpret_cast<float*>(base + w.partial);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(packed_chunks_kernel, dim3(1), dim3(1024), 0, st, row_off, n_groups, rows, w.kc, chunks, w.most,
+                     n_chunks, first, count);
+  const bool wide = rows_aligned(q, ldq, 1) && rows_aligned(B, ldb, type_bytes(type));
   with_type(type, [&](auto zero) {
     using T = decltype(zero);
-    hipLaunchKernelGGL(packed_wgrad_kernel<T>, dim3(cdiv(P, 64), cdiv(Q, 64), n_groups), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), q, ldq, code, ldc, static_cast<const T*>(B), ldb, P, Q,
-                       row_off, rows, G);
+    auto go = [&](auto is_wide) {
+      hipLaunchKernelGGL((packed_wgrad_kernel<T, decltype(is_wide)::value>), dim3((unsigned)blocks), dim3(256), 0, st, q,
+                         ldq, code, ldc, static_cast<const T*>(B), ldb, P, Q, chunks, n_chunks, w.tiles_p, w.tiles_q,
+                         partial, G);
+    };
+    if (wide) go(std::true_type{});
+    else go(std::false_type{});
   });
+  const int64_t PQ = (int64_t)P * Q;
+  hipLaunchKernelGGL(packed_reduce_kernel, dim3(cdiv(PQ, 1024) < 1024 ? cdiv(PQ, 1024) : 1024, n_groups), dim3(256), 0,
+                     st, partial, first, count, PQ, G);
   return launched();
 }
