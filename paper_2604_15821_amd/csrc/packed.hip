@@ -5,6 +5,8 @@
 // 2^-126, so the rounding (to nearest, ties to even) is off by at most half of it, max|x| / 127.  Code 255
 // stands for a block that held an infinity or NaN: all of it is NaN when read.
 // A power of two and seven bits fit bf16 exactly, so a product with a bf16 value is exact in fp32.
+#include <algorithm>
+
 #include "rows.h"
 
 namespace janus {
@@ -140,8 +142,8 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
 // with one term, else 128).  Both operands arrive with p and c, not m, along memory rows.  They are put into LDS as they
 // come, [32 m][p or c] in bf16, and read with the transposing ds_read_b64_tr_b16: 16 lanes give the addresses of
 // four rows of 16 values and receive four m of one column each, two reads an operand of the 32 x 32 x 16
-// instruction.  The 32-byte units of a row are stored at unit ^ (m % 8), so that the four rows of a read fall on
-// different banks.  Stages of 32 rows alternate between two LDS buffers, and the registers of a stage are
+// instruction.  The 32-byte units of a row are stored at unit ^ 2 (m % 4), so that the four rows and two units that 32
+// lanes read fall on different banks.  Stages of 32 rows alternate between two LDS buffers, and the registers of a stage are
 // loaded two stages before it is multiplied.
 //
 // Rows are cut into chunks, a group's longest first and given to the dies in turn, so that the tiles of a chunk
@@ -173,29 +175,35 @@ __device__ __forceinline__ unsigned pack_high(float a, float b) {   // the upper
 }
 __device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
 
-// Eight values of a row of B, and their planes.
+// Rows of a chunk as a buffer: reads behind its last value give zero, so a chunk's ragged end needs no code.
+typedef __amdgpu_buffer_rsrc_t buffer;
+__device__ __forceinline__ buffer rows_buffer(const void* p, unsigned bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
+}
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// Eight values of a row of B at byte `at`, and their planes.
 template <typename T>
 struct Octet {
   T v[8];
   template <bool WIDE>
-  __device__ __forceinline__ void load(const T* __restrict__ row, int c, int n) {
+  __device__ __forceinline__ void load(buffer b, unsigned at) {
     if constexpr (WIDE) {
       typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
       constexpr int V = 16 / (int)sizeof(T);
 #pragma unroll
-      for (int j = 0; j < 8; j += V) {   // a run that begins past the row reads the first one, and is not stored
-        const vec u = *reinterpret_cast<const vec*>(row + (c + j < n ? c + j : 0));
+      for (int j = 0; j < 8; j += V) {
+        const vec u = __builtin_bit_cast(vec, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at + j * sizeof(T), 0, 0));
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j + i] = u[i];
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = row[min(c + j, n - 1)];
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) v[j] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(b, at + 4 * j, 0, 0));
+        else v[j] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(b, at + 2 * j, 0, 0));
+      }
     }
-  }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (T)0.f;
   }
   __device__ __forceinline__ void planes(uint4 (&o)[Terms<T>::kPlanes]) const {
     if constexpr (Terms<T>::kPlanes == 1) {
@@ -218,26 +226,26 @@ struct Octet {
   }
 };
 
-// Sixteen packed values of a row and their scale, as bf16.
+// Sixteen packed values of a row and their code, as bf16.  (Behind the end both are zero: a scale of zero.)
 struct Sixteen {
-  uint4 q;
+  u32x4 q;
   int code;
   template <bool WIDE>
-  __device__ __forceinline__ void load(const int8_t* __restrict__ row, const uint8_t* __restrict__ codes, int c, int n) {
+  __device__ __forceinline__ void load(buffer b, unsigned at, buffer codes, unsigned at_code) {
     if constexpr (WIDE) {
-      q = *reinterpret_cast<const uint4*>(row + (c < n ? c : 0));
+      q = (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0);
     } else {
-      unsigned w[4] = {0u, 0u, 0u, 0u};
+      q = u32x4{};
 #pragma unroll
-      for (int j = 0; j < 16; ++j) w[j >> 2] |= (unsigned)(uint8_t)row[min(c + j, n - 1)] << (8 * (j & 3));
-      q = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int j = 0; j < 16; ++j)
+        q[j >> 2] |= (unsigned)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(b, at + j, 0, 0) << (8 * (j & 3));
     }
-    code = codes[min(c, n - 1) / kPackBlock];
+    code = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(codes, at_code, 0, 0);
   }
-  __device__ __forceinline__ void clear() { code = 0; }   // a scale of zero
-  __device__ __forceinline__ void values(uint4 (&o)[2]) const {
+  // the half `first` of them, then the other
+  __device__ __forceinline__ void values(int first, uint4 (&o)[2]) const {
     const float s = code_scale(code);
-    const unsigned in[4] = {q.x, q.y, q.z, q.w};
+    const unsigned in[4] = {first ? q.z : q.x, first ? q.w : q.y, first ? q.x : q.z, first ? q.y : q.w};
     unsigned w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -258,6 +266,16 @@ __device__ __forceinline__ bf16x8 read_columns(const char* lo, const char* hi) {
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo);
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi);
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Where a row's 32-byte unit lies.
+__device__ __forceinline__ int place(int unit, int m) { return unit ^ (2 * (m & 3)); }
+
+// Bytes of `rows` rows up to the last one's last value; where they are read by 16 bytes, rounded up to those.
+template <bool WIDE>
+__device__ __forceinline__ unsigned last_byte(int rows, long long ld, int width, int size) {
+  const unsigned n = (unsigned)(((rows - 1) * ld + width) * size);
+  return WIDE ? (n + 15) & ~15u : n;
 }
 
 template <typename T, bool WIDE>
@@ -282,38 +300,40 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
 
   // staging: thread t holds 16 values of X's row t / 8 and, per pass, 8 values of a row of B
-  const int ma = t >> 3, ua = t & 7, colA = p0 + 16 * ua;
-  const int wa = ma * kRowA + ((ua ^ (ma & 7)) << 5);
+  const int rows = ch.r1 - ch.r0;
+  const buffer bufA = rows_buffer(q + ch.r0 * ldq, last_byte<WIDE>(rows, ldq, P, 1));
+  const buffer bufC = rows_buffer(code + ch.r0 * ldc, last_byte<false>(rows, ldc, (P + kPackBlock - 1) / kPackBlock, 1));
+  const buffer bufB = rows_buffer(b + ch.r0 * ldb, last_byte<WIDE>(rows, ldb, Q, sizeof(T)));
+  const int ma = t >> 3, ua = t & 7, half = ma & 1;
+  const int wa = ma * kRowA + (place(ua, ma) << 5);
   constexpr int kPerRow = COLS / 8, kRowsPass = 256 / kPerRow;
-  const int mb = t / kPerRow, ob = t % kPerRow, colB = c0 + 8 * ob;
+  const int mb = t / kPerRow, ob = t % kPerRow;
+  unsigned atA = ma * (unsigned)ldq + p0 + 16 * ua, atC = ma * (unsigned)ldc + (p0 + 16 * ua) / kPackBlock;
+  unsigned atB = (mb * (unsigned)ldb + c0 + 8 * ob) * (unsigned)sizeof(T);
+  const unsigned stepB = kWgRows * (unsigned)ldb * (unsigned)sizeof(T), passB = stepB / (32 / kRowsPass);
   struct Regs {
     Sixteen a;
     Octet<T> b[kPass];
   };
-  auto load = [&](Regs& r, int m0) {
-    const long long ra = min(m0 + ma, ch.r1 - 1);
-    r.a.template load<WIDE>(q + ra * ldq, code + ra * ldc, colA, P);
+  auto load = [&](Regs& r) {   // the next stage's values
+    r.a.template load<WIDE>(bufA, atA, bufC, atC);
 #pragma unroll
-    for (int i = 0; i < kPass; ++i)
-      r.b[i].template load<WIDE>(b + (long long)min(m0 + mb + i * kRowsPass, ch.r1 - 1) * ldb, colB, Q);
+    for (int i = 0; i < kPass; ++i) r.b[i].template load<WIDE>(bufB, atB + i * passB);
+    atA += kWgRows * (unsigned)ldq;
+    atC += kWgRows * (unsigned)ldc;
+    atB += stepB;
   };
-  auto stage = [&](Regs& r, int m0, char* to) {
-    if (m0 + kWgRows > ch.r1) {   // rows past the end count as zero
-      if (m0 + ma >= ch.r1) r.a.clear();
-#pragma unroll
-      for (int i = 0; i < kPass; ++i)
-        if (m0 + mb + i * kRowsPass >= ch.r1) r.b[i].clear();
-    }
-    uint4 o[2];
-    r.a.values(o);
-    *reinterpret_cast<uint4*>(to + wa) = o[0];
-    *reinterpret_cast<uint4*>(to + wa + 16) = o[1];
+  auto stage = [&](const Regs& r, char* to) {
+    uint4 o[2];   // odd rows write their second half first: two rows then fill all banks
+    r.a.values(half, o);
+    *reinterpret_cast<uint4*>(to + wa + 16 * half) = o[0];
+    *reinterpret_cast<uint4*>(to + wa + 16 - 16 * half) = o[1];
 #pragma unroll
     for (int i = 0; i < kPass; ++i) {
       const int m = mb + i * kRowsPass;
       uint4 w[NP];
       r.b[i].planes(w);
-      char* at_b = to + kBytesA + m * kRowB + (((ob >> 1) ^ (m & 7)) << 5) + ((ob & 1) << 4);
+      char* at_b = to + kBytesA + m * kRowB + (place(ob >> 1, m) << 5) + ((ob & 1) << 4);
 #pragma unroll
       for (int n = 0; n < NP; ++n) *reinterpret_cast<uint4*>(at_b + n * kBytesB) = w[n];
     }
@@ -326,10 +346,10 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   for (int h = 0; h < 2; ++h) {
     const int m = 8 * (g >> 1) + 4 * h + r;
 #pragma unroll
-    for (int f = 0; f < 2; ++f) fa[f][h] = m * kRowA + ((((wave >> 1) * 4 + 2 * f + (g & 1)) ^ (m & 7)) << 5) + sub;
+    for (int f = 0; f < 2; ++f) fa[f][h] = m * kRowA + (place((wave >> 1) * 4 + 2 * f + (g & 1), m) << 5) + sub;
 #pragma unroll
     for (int f = 0; f < kFrag; ++f)
-      fb[f][h] = kBytesA + m * kRowB + ((((wave & 1) * (COLS / 32) + 2 * f + (g & 1)) ^ (m & 7)) << 5) + sub;
+      fb[f][h] = kBytesA + m * kRowB + (place((wave & 1) * (COLS / 32) + 2 * f + (g & 1), m) << 5) + sub;
   }
   f32x16 acc[2][kFrag];
 #pragma unroll
@@ -355,21 +375,21 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   };
 
   Regs r0, r1;
-  const int steps = (ch.r1 - ch.r0 + kWgRows - 1) / kWgRows;
-  load(r0, ch.r0);
-  stage(r0, ch.r0, lds);
-  load(r0, ch.r0 + kWgRows);
+  const int steps = (rows + kWgRows - 1) / kWgRows;
+  load(r0);
+  stage(r0, lds);
+  load(r0);
   __syncthreads();
-  auto step = [&](int s, Regs& next, Regs& after) {   // multiplies stage s; `next` holds stage s + 1
-    const int m = ch.r0 + s * kWgRows;
-    load(after, m + 2 * kWgRows);
-    multiply(lds + (s & 1) * kStage);
-    stage(next, m + kWgRows, lds + ((s + 1) & 1) * kStage);
+  // multiplies the stage in `from` while r holds the next one and the one after is loaded
+  auto step = [&](const char* from, char* to, Regs& next, Regs& after) {
+    load(after);
+    multiply(from);
+    stage(next, to);
     __syncthreads();
   };
   for (int s = 0; s < steps; s += 2) {
-    step(s, r0, r1);
-    if (s + 1 < steps) step(s + 1, r1, r0);
+    step(lds, lds + kStage, r0, r1);
+    if (s + 1 < steps) step(lds + kStage, lds, r1, r0);
   }
 
   float* out = ch.alone ? G + (long long)ch.group * P * Q : partial + (long long)at * P * Q;
@@ -443,13 +463,15 @@ struct WgradPlan {
   int64_t chunks, first, count, partial, total;   // offsets in bytes
 };
 // The chunk length: half of what each of 512 resident workgroups would get of all stages, so that the last ones end
-// together; not below 256 rows, where partials cost more than they save.
+// together; not below 256 rows, where partials cost more than they save, nor above 16 384, so that a chunk's
+// bytes stay within the 32-bit offsets of a buffer for rows of up to 256 KB.
+constexpr int kMostChunkRows = 16384;
 static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
   WgradPlan w;
   w.tiles_p = (int)cdiv(P, kWgP);
   w.tiles_q = (int)cdiv(Q, type == JANUS_BF16 ? Terms<__bf16>::kCols : Terms<float>::kCols);
   const double share = (double)rows * w.tiles_p * w.tiles_q / 1024;
-  const double kc = share < 256 ? 256 : share > 1e9 ? 1e9 : share;
+  const double kc = share < 256 ? 256 : share > kMostChunkRows ? kMostChunkRows : share;
   w.kc = (int)((kc + kWgRows - 1) / kWgRows) * kWgRows;
   w.most = (int)(groups + rows / w.kc);
   w.chunks = 16;
@@ -549,7 +571,8 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
     return JANUS_EINVAL;
   const WgradPlan w = wgrad_plan(rows, n_groups, P, Q, type);
   const int64_t blocks = ((int64_t)w.most + 7) / 8 * 8 * w.tiles_p * w.tiles_q;
-  if (blocks > INT_MAX) return JANUS_EUNSUPPORTED;
+  const int64_t row_bytes = std::max({ldq, ldc, ldb * type_bytes(type)});
+  if (blocks > INT_MAX || (rows > 0 && row_bytes > (int64_t)UINT_MAX / (w.kc + 4 * kWgRows))) return JANUS_EUNSUPPORTED;
   char* base = static_cast<char*>(work);
   int* n_chunks = reinterpret_cast<int*>(base);
   PackedChunk* chunks = reinterpret_cast<PackedChunk*>(base + w.chunks);
