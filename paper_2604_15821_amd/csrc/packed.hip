@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
 // come, [32 m][p or c] in bf16, and read with the transposing ds_read_b64_tr_b16: 16 lanes give the addresses of
 // four rows of 16 values and receive four m of one column each, two reads an operand of the 32 x 32 x 16
 // instruction.  The 32-byte units of a row are stored at unit ^ 2 (m % 4), so that the four rows and two units that 32
-// lanes read fall on different banks.  Stages of 32 rows alternate between two LDS buffers, and the registers of a stage are
+// lanes read fall on different banks.  Stages of 32 rows alternate between two LDS buffers, and a stage's registers are
 // loaded two stages before it is multiplied.
 //
 // Rows are cut into chunks, a group's longest first and given to the dies in turn, so that the tiles of a chunk
@@ -274,7 +274,7 @@ __device__ __forceinline__ int place(int unit, int m) { return unit ^ (2 * (m & 
 // Bytes of `rows` rows up to the last one's last value; where they are read by 16 bytes, rounded up to those.
 template <bool WIDE>
 __device__ __forceinline__ unsigned last_byte(int rows, long long ld, int width, int size) {
-  const unsigned n = (unsigned)(((rows - 1) * ld + width) * size);
+  const unsigned n = rows ? (unsigned)(((rows - 1) * ld + width) * size) : 0u;
   return WIDE ? (n + 15) & ~15u : n;
 }
 
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   stage(r0, lds);
   load(r0);
   __syncthreads();
-  // multiplies the stage in `from` while r holds the next one and the one after is loaded
+  // multiplies the stage in `from` while `next` holds the one after it and `after` is loaded with the next but one
   auto step = [&](const char* from, char* to, Regs& next, Regs& after) {
     load(after);
     multiply(from);
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(1024) void packed_chunks_kernel(const int* __restri
                                                              int kc, PackedChunk* __restrict__ chunks, int most,
                                                              int* __restrict__ n_chunks, int* __restrict__ first,
                                                              int* __restrict__ count) {
-  __shared__ int len[1024], n[1024];
+  __shared__ int2 size_n[1024];   // rows per chunk, chunks
   const int g = threadIdx.x;
   int a = 0, size = 0;
   if (g < groups) {
@@ -425,35 +425,46 @@ __global__ __launch_bounds__(1024) void packed_chunks_kernel(const int* __restri
   }
   const int mine = (size + kc - 1) / kc;
   const int each = mine ? ((size + mine - 1) / mine + kWgRows - 1) / kWgRows * kWgRows : 0;
-  n[g] = mine ? (size + each - 1) / each : 0;
-  len[g] = each;
+  const int n = g >= groups ? 0 : mine ? (size + each - 1) / each : 1;   // a group without rows: one empty chunk
+  size_n[g] = make_int2(each, n);
   __syncthreads();
   int at = 0, all = 0;
-  for (int o = 0; o < groups; ++o) {
-    at += len[o] > len[g] || (len[o] == len[g] && o < g) ? n[o] : 0;
-    all += n[o];
+  if (g < groups) {
+#pragma unroll 8
+    for (int o = 0; o < groups; ++o) {
+      const int2 v = size_n[o];
+      at += v.x > each || (v.x == each && o < g) ? v.y : 0;
+      all += v.y;
+    }
   }
   if (g < groups) {
     first[g] = at;
-    const int held = min(n[g], max(most - at, 0));   // fewer only where offsets overlap
+    const int held = min(n, max(most - at, 0));   // fewer only where offsets overlap
     count[g] = held;
     for (int i = 0; i < held; ++i)
-      chunks[at + i] = PackedChunk{g, a + i * each, a + (int)min((i + 1ll) * each, (long long)size), n[g] == 1};
+      chunks[at + i] = PackedChunk{g, a + i * each, a + (int)min((i + 1ll) * each, (long long)size), n == 1};
   }
   if (g == 0) *n_chunks = min(all, most);
 }
 
-// Adds the partials of groups with several chunks, in order, and clears groups with none.
+// Adds the partials of groups with several chunks, in order, four in flight.
 __global__ __launch_bounds__(256) void packed_reduce_kernel(const float* __restrict__ partial,
                                                             const int* __restrict__ first,
                                                             const int* __restrict__ count, long long PQ,
                                                             float* __restrict__ G) {
   const int g = blockIdx.y, n = count[g];
-  if (n == 1) return;
+  if (n < 2) return;
   const float* p = partial + first[g] * PQ;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < PQ; i += (long long)gridDim.x * 256) {
     float v = 0.f;
-    for (int k = 0; k < n; ++k) v += p[k * PQ + i];
+    for (int k = 0; k < n; k += 4) {
+      float u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) u[j] = p[min(k + j, n - 1) * PQ + i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k + j < n) v += u[j];
+    }
     G[g * PQ + i] = v;
   }
 }
@@ -463,7 +474,8 @@ struct WgradPlan {
   int64_t chunks, first, count, partial, total;   // offsets in bytes
 };
 // The chunk length: half of what each of 512 resident workgroups would get of all stages, so that the last ones end
-// together; not below 256 rows, where partials cost more than they save, nor above 16 384, so that a chunk's
+// together; not below 512 rows, where partials cost more than they save (20 000 rows, one group, 256 x 256, fp32: 37 us at 256,
+// 30 at 512), nor above 16 384, so that a chunk's
 // bytes stay within the 32-bit offsets of a buffer for rows of up to 256 KB.
 constexpr int kMostChunkRows = 16384;
 static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
@@ -471,7 +483,7 @@ static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
   w.tiles_p = (int)cdiv(P, kWgP);
   w.tiles_q = (int)cdiv(Q, type == JANUS_BF16 ? Terms<__bf16>::kCols : Terms<float>::kCols);
   const double share = (double)rows * w.tiles_p * w.tiles_q / 1024;
-  const double kc = share < 256 ? 256 : share > kMostChunkRows ? kMostChunkRows : share;
+  const double kc = share < 512 ? 512 : share > kMostChunkRows ? kMostChunkRows : share;
   w.kc = (int)((kc + kWgRows - 1) / kWgRows) * kWgRows;
   w.most = (int)(groups + rows / w.kc);
   w.chunks = 16;
@@ -594,7 +606,8 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
     else go(std::false_type{});
   });
   const int64_t PQ = (int64_t)P * Q;
-  hipLaunchKernelGGL(packed_reduce_kernel, dim3(cdiv(PQ, 1024) < 1024 ? cdiv(PQ, 1024) : 1024, n_groups), dim3(256), 0,
-                     st, partial, first, count, PQ, G);
+  if (rows > w.kc)   // else no group has several chunks
+    hipLaunchKernelGGL(packed_reduce_kernel, dim3(cdiv(PQ, 256) < 1024 ? cdiv(PQ, 256) : 1024, n_groups), dim3(256),
+                       0, st, partial, first, count, PQ, G);
   return launched();
 }
