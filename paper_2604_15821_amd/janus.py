@@ -13,6 +13,7 @@ from dataclasses import dataclass
 from typing import NamedTuple
 
 import numpy as np
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "libjanus.so")
@@ -526,16 +527,13 @@ def grouped_gemm_noalloc(A, B, row_off, K, N, trans_b, out):
 ACT = {"none": 0, "silu": 1}
 
 
-def _types():
-    import torch
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def _type_of(t, name):
     """janus_type of a tensor or of a torch dtype."""
-    import torch
     dt = t.dtype if isinstance(t, torch.Tensor) else t
-    code = _types().get(dt)
+    code = _TYPES.get(dt)
     if code is None:
         raise TypeError(f"{name}: {dt}, expected float32, bfloat16 or float16")
     return code
@@ -543,12 +541,11 @@ def _type_of(t, name):
 
 def _rows(t, name, dtype, shape, device):
     """Check a [rows, width] tensor whose rows may lie apart; returns (address, row distance)."""
-    import torch
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if t.dtype != dtype:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if not t.is_cuda or t.device != device:
         raise ValueError(f"{name}: on {t.device}, expected a device tensor on {device}")
@@ -571,7 +568,6 @@ def _param(t, name, d, device):
 
 
 def _matrix(t, name):
-    import torch
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if t.dim() != 2:
@@ -587,11 +583,11 @@ class _on:
         self.device, self.guard = device, None
 
     def __enter__(self):
-        import torch
         if torch.cuda.current_device() != self.device.index:
             self.guard = torch.cuda.device(self.device)
             self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        # the handle itself: current_stream() builds an object around it, 3 us of a call of 12
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def __exit__(self, *e):
         if self.guard is not None:
@@ -632,7 +628,6 @@ def residual_norm(x, b, w_post=None, gate=None, gate_off=None, scale=None, w_pre
     [n_seq + 1] int32 (rows behind the last sequence are left alone: zero in new outputs, as they
     were in `out`).  Returns (r, n), n None without w_pre; out = (r, n) to write into, where r may be x and
     n may be b."""
-    import torch
     rows, d, dev = _matrix(b, "b")
     pb, ldb = _rows(b, "b", b.dtype, (rows, d), dev)
     px, ldx = _rows(x, "x", b.dtype, (rows, d), dev)
@@ -666,7 +661,6 @@ def residual_norm_grad(dr, dn, r, b, w_post=None, gate=None, gate_off=None, scal
     """Gradients of residual_norm in all its inputs, at the stored r and b, from the gradients dr and
     dn of its outputs (dr None: zero; dn and r None without w_pre).  out = (dx, db) to write into, where
     dx may be dr and db may be dn.  Rows behind the last sequence add to no gradient."""
-    import torch
     rows, d, dev = _matrix(b, "b")
     dt = b.dtype
     like = lambda t, name: (None, 0) if t is None else _rows(t, name, dt, (rows, d), dev)  # noqa: E731
@@ -686,8 +680,8 @@ def residual_norm_grad(dr, dn, r, b, w_post=None, gate=None, gate_off=None, scal
         dx, db = out
     pdx, lddx = _rows(dx, "dx", dt, (rows, d), dev)
     pdb, lddb = _rows(db, "db", dt, (rows, d), dev)
-    param = lambda w: None if w is None else torch.empty(d, dtype=torch.float32, device=dev)  # noqa: E731
-    dw_post, dscale, dw_pre = param(w_post), param(scale), param(w_pre)
+    dw = iter(torch.empty(3, d, dtype=torch.float32, device=dev))
+    dw_post, dscale, dw_pre = (None if w is None else next(dw) for w in (w_post, scale, w_pre))
     dgate = None if gate is None else torch.empty(gate.shape, dtype=dt, device=dev)
     adr = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
     lib = _lib()
@@ -707,7 +701,6 @@ def expert_layer(x, router, w_up, w_down, top_k, beta=None, normalize=False, out
 
     router [d, n] float32, beta [n] float32 or None, w_up [n, d, h] and w_down [n, h, d] of x's type; d and h
     multiples of 16.  Returns (y [tokens, d], expert ids [tokens, top_k] int32, gates float32)."""
-    import torch
     tokens, d, dev = _matrix(x, "x")
     if not isinstance(w_up, torch.Tensor) or w_up.dim() != 3:
         raise ValueError("w_up: expected a tensor [experts, d, hidden]")
@@ -747,7 +740,6 @@ class PackedRows(NamedTuple):
 
 
 def _packed(p, device=None):
-    import torch
     rows, d, dev = _matrix(p.q, "q")
     if device is not None and dev != device:
         raise ValueError(f"q: on {dev}, expected {device}")
@@ -759,7 +751,6 @@ def _packed(p, device=None):
 def pack_rows(x, out=None) -> PackedRows:
     """x [rows, d] (float32, bfloat16 or float16) in 8 bits.  The values' rows start on multiples of 16 bytes;
     out = PackedRows to write into."""
-    import torch
     rows, d, dev = _matrix(x, "x")
     code = _type_of(x, "x")
     px, ldx = _rows(x, "x", x.dtype, (rows, d), dev)
@@ -780,7 +771,6 @@ def unpack_rows(packed, dtype, act="none", grad=None, value=None, out=None):
     act "none": returns X.  act "silu": returns SiLU(X), or with grad [rows, d] the gradient
     grad * SiLU'(X), or with grad and value=True both as (gradient, SiLU(X)).  `out`: tensor for the
     first result (it may be grad)."""
-    import torch
     rows, d, dev, at = _packed(packed)
     code = _type_of(dtype, "dtype")
     if act not in ACT:
@@ -804,7 +794,6 @@ def packed_wgrad(packed, B, row_off, out=None):
     """Grouped weight gradient from activations in 8 bits: G_g = X_g^T B_g over the rows
     row_off[g] .. row_off[g + 1] - 1 of X (packed [rows, P]) and B [rows, Q] (float32, bfloat16 or
     float16); returns G [groups, P, Q] float32.  row_off [groups + 1] int32 on the device."""
-    import torch
     rows, P, dev, at = _packed(packed)
     n, Q, _ = _matrix(B, "B")
     code = _type_of(B, "B")
