@@ -183,7 +183,7 @@ __global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_kernel(
 }
 
 template <typename T, int L, int C, bool VEC>
-__global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_grad_kernel(
+__global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 4 : 2)) void residual_norm_grad_kernel(
     NormArgs a, const T* dr, long long lddr, const T* dn, long long lddn, const T* r, long long ldr, const T* b,
     long long ldb, T* dx, long long lddx, T* db, long long lddb, NormGradOut o, long long run) {
   using R = Row<T, L, C, VEC>;
@@ -319,42 +319,55 @@ __global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_grad_kernel
   if (a.w_post || a.scale) join(Q, out + a.d);
 }
 
-// Adds the partials.  Workgroups with blockIdx.y = 0 own 32 columns of dw_pre and of Q: eight slices
-// of each take every eighth partial and are added in order.  The others own sequences whose
-// rows lie in several runs, and clear the gradients of sequences without rows.
-template <typename T>
-__global__ __launch_bounds__(512) void residual_norm_finish_kernel(NormArgs a, NormGradOut o, int parts,
-                                                                   long long run, float* dw_post, float* dscale,
-                                                                   float* dw_pre) {
-  if (blockIdx.y == 0) {
-    __shared__ float red[2][8][32];
-    const int cl = threadIdx.x & 31, sl = (threadIdx.x >> 5) & 7, which = threadIdx.x >> 8;
-    for (int c0 = blockIdx.x * 32; c0 < a.d; c0 += gridDim.x * 32) {
-      const int c = c0 + cl;
-      const bool on = c < a.d && (which ? a.w_post || a.scale : a.w_pre != nullptr);
-      float s = 0.f;
-      if (on)
-        for (int p = sl; p < parts; p += 8) s += o.partial[((long long)p * 2 + which) * a.d + c];
-      red[which][sl][cl] = s;
-      __syncthreads();
-      if (sl == 0 && on) {
-        float v = 0.f;
+// Adds n values `stride` floats apart in order, eight in flight.
+__device__ __forceinline__ float sum_apart(const float* p, long long stride, int n) {
+  float s = 0.f;
+  for (int i = 0; i < n; i += 8) {
+    float u[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v += red[which][q][cl];
-        if (which == 0) {
-          if (dw_pre) dw_pre[c] = v;
-        } else {
-          if (dw_post) dw_post[c] = v * (a.scale ? a.scale[c] : 1.f);
-          if (dscale) dscale[c] = v * (a.w_post ? a.w_post[c] : 1.f);
-        }
+    for (int j = 0; j < 8; ++j) u[j] = p[min(i + j, n - 1) * stride];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j < n) s += u[j];
+  }
+  return s;
+}
+
+// Adds the partials.  Workgroups with blockIdx.y = 0 (dw_pre) and 1 (Q) own 16 columns; 32 slices of consecutive
+// partials are added in order.  The others own sequences whose rows lie in several runs, and clear the gradients
+// of sequences without rows.
+constexpr int kFinishSlices = 32;
+template <typename T>
+__global__ __launch_bounds__(16 * kFinishSlices) void residual_norm_finish_kernel(NormArgs a, NormGradOut o, int parts,
+                                                                                  long long run, float* dw_post,
+                                                                                  float* dscale, float* dw_pre) {
+  if (blockIdx.y < 2) {
+    __shared__ float red[kFinishSlices][16];
+    const bool pre = blockIdx.y == 0;
+    if (pre ? !dw_pre : !dw_post && !dscale) return;
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), sl = threadIdx.x >> 4;
+    const int each = (parts + kFinishSlices - 1) / kFinishSlices, p0 = sl * each;
+    float s = 0.f;
+    if (c < a.d && p0 < parts)
+      s = sum_apart(o.partial + ((long long)p0 * 2 + !pre) * a.d + c, 2ll * a.d, min(each, parts - p0));
+    red[sl][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (sl == 0 && c < a.d) {
+      s = 0.f;
+#pragma unroll
+      for (int q = 0; q < kFinishSlices; ++q) s += red[q][threadIdx.x];
+      if (pre) {
+        dw_pre[c] = s;
+      } else {
+        if (dw_post) dw_post[c] = s * (a.scale ? a.scale[c] : 1.f);
+        if (dscale) dscale[c] = s * (a.w_post ? a.w_post[c] : 1.f);
       }
-      __syncthreads();
     }
     return;
   }
   T* dgate = static_cast<T*>(o.dgate);
   const long long limit = norm_limit(a);
-  for (int s = blockIdx.x + gridDim.x * (blockIdx.y - 1); s < a.n_seq; s += gridDim.x * (gridDim.y - 1)) {
+  for (int s = blockIdx.x + gridDim.x * (blockIdx.y - 2); s < a.n_seq; s += gridDim.x * (gridDim.y - 2)) {
     const long long m0 = max((long long)a.gate_off[s], 0ll), m1 = min((long long)a.gate_off[s + 1], limit);
     const bool empty = m1 <= m0;
     const long long w0 = empty ? 0 : m0 / run, w1 = empty ? 0 : (m1 - 1) / run;
@@ -362,8 +375,7 @@ __global__ __launch_bounds__(512) void residual_norm_finish_kernel(NormArgs a, N
     for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
       float v = 0.f;
       if (!empty) {
-        v = o.part_seq[(2 * w0 + 1) * a.d + c];
-        for (long long w = w0 + 1; w <= w1; ++w) v += o.part_seq[2 * w * a.d + c];
+        v = o.part_seq[(2 * w0 + 1) * a.d + c] + sum_apart(o.part_seq + 2 * (w0 + 1) * a.d + c, 2ll * a.d, (int)(w1 - w0));
         if (a.scale) v *= a.scale[c];
         if (a.w_post) v *= a.w_post[c];
       }
@@ -372,17 +384,19 @@ __global__ __launch_bounds__(512) void residual_norm_finish_kernel(NormArgs a, N
   }
 }
 
-// Lanes and columns per lane of a width, as the first that hold it.
+// Lanes per row of a width (with 8 or 16 columns per lane, the first that hold it), and the workgroups that the
+// backward kernel's registers let a CU hold, as which it is launched at most: more would run as a
+// second, shorter round and write more partials.
 struct NormShape {
-  int lanes, cols;
+  int lanes, resident;
 };
 static NormShape norm_shape(int d) {
-  if (d <= 128) return {16, 8};
-  if (d <= 512) return {64, 8};
-  if (d <= 1024) return {64, 16};
-  if (d <= 2048) return {256, 8};
-  if (d <= 4096) return {256, 16};
-  return {512, 16};
+  if (d <= 128) return {16, 4};
+  if (d <= 512) return {64, 4};
+  if (d <= 1024) return {64, 2};
+  if (d <= 2048) return {256, 4};
+  if (d <= 4096) return {256, 2};
+  return {512, 1};
 }
 
 template <typename F>
@@ -407,7 +421,8 @@ static NormPlan norm_plan(long long rows, int d, int target) {
   const long long groups = (rows + run - 1) / run;
   return {run, (int)((groups + per - 1) / per), per};
 }
-constexpr int kForwardBlocks = 4096, kGradBlocks = 1024;
+constexpr int kForwardBlocks = 4096;
+static int grad_blocks(int d) { return 256 * norm_shape(d).resident; }
 
 static int check_norm(const janus_norm* p) {
   if (!p || p->rows < 0 || p->rows > INT_MAX || p->d < 1 || !type_known(p->type) || !(p->eps >= 0.f) ||
@@ -466,7 +481,7 @@ extern "C" int janus_residual_norm(const janus_norm* p, const void* x, int64_t l
 extern "C" int64_t janus_residual_norm_grad_workspace(const janus_norm* p) {
   int rc = check_norm(p);
   if (rc) return rc;
-  const NormPlan plan = norm_plan(p->rows, p->d, kGradBlocks);
+  const NormPlan plan = norm_plan(p->rows, p->d, grad_blocks(p->d));
   int64_t floats = (int64_t)plan.blocks * 2 * p->d;
   if (p->gate_off) floats += (int64_t)plan.blocks * plan.groups_per_block * 2 * p->d;
   return 4 * floats + 16;
@@ -492,7 +507,7 @@ extern "C" int janus_residual_norm_grad(const janus_norm* p, const void* dr, int
                    rows_aligned(b, ldb, e) && rows_aligned(dx, lddx, e) && rows_aligned(db, lddb, e) &&
                    rows_aligned(dgate, lddg, e);
   const NormArgs a = norm_args(p);
-  const NormPlan plan = norm_plan(p->rows, p->d, kGradBlocks);
+  const NormPlan plan = norm_plan(p->rows, p->d, grad_blocks(p->d));
   NormGradOut o{static_cast<float*>(work), nullptr, dgate, lddg};
   o.part_seq = o.partial + (int64_t)plan.blocks * 2 * p->d;
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -513,10 +528,10 @@ extern "C" int janus_residual_norm_grad(const janus_norm* p, const void* dr, int
       });
     const bool sums = dw_post || dscale || dw_pre, seqs = dgate && a.gate_off && a.n_seq > 0;
     if (sums || seqs) {
-      const int bx = (int)cdiv(p->d, 32);
-      const int by = seqs ? 1 + (int)cdiv(a.n_seq < 2048 ? a.n_seq : 2048, bx) : 1;
-      hipLaunchKernelGGL(residual_norm_finish_kernel<T>, dim3(bx, by), dim3(512), 0, st, a, o, plan.blocks, plan.run,
-                         dw_post, dscale, dw_pre);
+      const int bx = (int)cdiv(p->d, 16);
+      const int by = seqs ? 2 + (int)cdiv(a.n_seq < 2048 ? a.n_seq : 2048, bx) : 2;
+      hipLaunchKernelGGL(residual_norm_finish_kernel<T>, dim3(bx, by), dim3(16 * kFinishSlices), 0, st, a, o, plan.blocks,
+                         plan.run, dw_post, dscale, dw_pre);
     }
   });
   return launched();
