@@ -64,6 +64,21 @@ struct Row {
       }
     }
   }
+  // a row's values as they are stored, to be taken apart later
+  struct Raw {
+    typedef T vec __attribute__((ext_vector_type(V)));
+    vec v[C / V];
+    __device__ __forceinline__ void load(const T* p, int lane, int d) {
+#pragma unroll
+      for (int i = 0; i < C / V; ++i) v[i] = *reinterpret_cast<const vec*>(p + min(col(i, lane), d - V));
+    }
+    __device__ __forceinline__ void values(float (&o)[C], int lane, int d) const {
+#pragma unroll
+      for (int i = 0; i < C / V; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[i * V + j] = col(i, lane) < d ? (float)v[i][j] : 0.f;
+    }
+  };
   template <typename S>
   static __device__ __forceinline__ void store(S* p, const float (&v)[C], int lane, int d) {
 #pragma unroll
@@ -183,7 +198,7 @@ __global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_kernel(
 }
 
 template <typename T, int L, int C, bool VEC>
-__global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 4 : 2)) void residual_norm_grad_kernel(
+__global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residual_norm_grad_kernel(
     NormArgs a, const T* dr, long long lddr, const T* dn, long long lddn, const T* r, long long ldr, const T* b,
     long long ldb, T* dx, long long lddx, T* db, long long lddb, NormGradOut o, long long run) {
   using R = Row<T, L, C, VEC>;
@@ -226,19 +241,32 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 4 : 2)) void residua
 #pragma unroll
     for (int j = 0; j < C; ++j) t[j] = 0.f;
   };
+  typename R::Raw ahead_b, ahead_dr, ahead_r, ahead_dn;   // the next row, where there are registers for it
+  auto fetch = [&](long long m) {
+    ahead_b.load(b + m * ldb, lane, a.d);
+    if (dr) ahead_dr.load(dr + m * lddr, lane, a.d);
+    if (a.w_pre) {
+      ahead_r.load(r + m * ldr, lane, a.d);
+      ahead_dn.load(dn + m * lddn, lane, a.d);
+    }
+  };
+  constexpr bool kAhead = C == 8 || sizeof(T) == 2;
+  if (kAhead && r0 < r1) fetch(r0);
   for (long long m = r0; m < r1; ++m) {
     float D[C], bv[C], rv[C], nv[C];
-    R::load(b + m * ldb, bv, lane, a.d);
+    if (!kAhead) fetch(m);
+    ahead_b.values(bv, lane, a.d);
     if (dr) {
-      R::load(dr + m * lddr, D, lane, a.d);
+      ahead_dr.values(D, lane, a.d);
     } else {
 #pragma unroll
       for (int j = 0; j < C; ++j) D[j] = 0.f;
     }
     if (a.w_pre) {
-      R::load(r + m * ldr, rv, lane, a.d);
-      R::load(dn + m * lddn, nv, lane, a.d);
+      ahead_r.values(rv, lane, a.d);
+      ahead_dn.values(nv, lane, a.d);
     }
+    if (kAhead && m + 1 < r1) fetch(m + 1);
     if (a.gate) {
       if (!a.gate_off) {
         R::load(gate + m * a.ldg, g, lane, a.d);
@@ -391,10 +419,10 @@ struct NormShape {
   int lanes, resident;
 };
 static NormShape norm_shape(int d) {
-  if (d <= 128) return {16, 4};
-  if (d <= 512) return {64, 4};
+  if (d <= 128) return {16, 3};
+  if (d <= 512) return {64, 3};
   if (d <= 1024) return {64, 2};
-  if (d <= 2048) return {256, 4};
+  if (d <= 2048) return {256, 3};
   if (d <= 4096) return {256, 2};
   return {512, 1};
 }
