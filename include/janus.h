@@ -523,10 +523,10 @@ int32_t janus_wgrad_chunk_rows(int64_t M, int32_t P, int32_t Q);
  * Arrays are row-major with a distance of ld* elements between rows (at least their width;
  * checked).  Element types are those of janus_type; sums, statistics and everything between
  * input and output are held in fp32, and outputs are rounded once (to nearest, ties to even).
- * Every address is a multiple of its element's size.  Where all rows start on multiples of 16
- * bytes (packed values: see there) and widths are multiples of 16 bytes, loads and stores are
- * 16 bytes wide; other layouts give the same results more slowly.  No kernel uses atomics on
- * floating-point values; results are the same on every run.
+ * Every address is a multiple of its element's size.  Rows that start on multiples of 16 bytes and
+ * widths that are multiples of 16 bytes are read and written fastest; other layouts give the same
+ * values.  Squares are summed in fp32: magnitudes stay below 1e18.  No kernel uses atomics on floating-point
+ * values; results are the same on every run.
  */
 typedef enum janus_type { JANUS_F32 = 0, JANUS_BF16 = 1, JANUS_F16 = 2 } janus_type;
 typedef enum janus_act { JANUS_ACT_NONE = 0, JANUS_ACT_SILU = 1 } janus_act;

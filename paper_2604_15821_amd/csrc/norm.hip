@@ -45,47 +45,66 @@ struct NormGradOut {
   long long lddg;
 };
 
-template <typename T, int L, int C, bool VEC>
+// The columns of a lane: C in runs of 16 bytes and, where d is no multiple of a run (ODD), one of the rest.
+template <typename T, int L, int C, bool ODD>
 struct Row {
-  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+  static constexpr int V = 16 / (int)sizeof(T), N = C + ODD;
   static constexpr int kThreads = L < 256 ? 256 : L;
   static constexpr int kGroups = kThreads / L;
   static __device__ __forceinline__ int col(int i, int lane) { return (i * L + lane) * V; }
-  // columns past the end read the last whole run and become zero, so that no load is behind a branch
+  static __device__ __forceinline__ int whole(int d) { return ODD ? d / V * V : d; }   // columns in runs
+  // Runs and rests past the end read the last ones and become zero, so that no load is behind a branch of a lane.
   template <typename S>
-  static __device__ __forceinline__ void load(const S* p, float (&v)[C], int lane, int d) {
+  static __device__ __forceinline__ void load(const S* p, float (&v)[N], int lane, int d) {
+    const int w = whole(d);
+    if (!ODD || w > 0) {
 #pragma unroll
-    for (int i = 0; i < C / V; ++i) {
-      const int c = col(i, lane);
-      load_run<S, V>(p + min(c, d - V), v + i * V);
-      if (c >= d) {
+      for (int i = 0; i < C / V; ++i) load_run<S, V>(p + min(col(i, lane), w - V), v + i * V);
+    }
+    if (ODD) v[C] = (float)p[min(w + lane, d - 1)];
+    trim(v, lane, d);
+  }
+  static __device__ __forceinline__ void trim(float (&v)[N], int lane, int d) {
+    const int w = whole(d);
+#pragma unroll
+    for (int i = 0; i < C / V; ++i)
+      if (col(i, lane) >= w) {
 #pragma unroll
         for (int j = 0; j < V; ++j) v[i * V + j] = 0.f;
       }
-    }
+    if (ODD && w + lane >= d) v[C] = 0.f;
   }
   // a row's values as they are stored, to be taken apart later
   struct Raw {
-    typedef T vec __attribute__((ext_vector_type(V)));
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     vec v[C / V];
+    T rest;
     __device__ __forceinline__ void load(const T* p, int lane, int d) {
+      const int w = whole(d);
+      if (!ODD || w > 0) {
 #pragma unroll
-      for (int i = 0; i < C / V; ++i) v[i] = *reinterpret_cast<const vec*>(p + min(col(i, lane), d - V));
+        for (int i = 0; i < C / V; ++i) v[i] = *reinterpret_cast<const vec*>(p + min(col(i, lane), w - V));
+      }
+      if (ODD) rest = p[min(w + lane, d - 1)];
     }
-    __device__ __forceinline__ void values(float (&o)[C], int lane, int d) const {
+    __device__ __forceinline__ void values(float (&o)[N], int lane, int d) const {
 #pragma unroll
       for (int i = 0; i < C / V; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[i * V + j] = col(i, lane) < d ? (float)v[i][j] : 0.f;
+        for (int j = 0; j < V; ++j) o[i * V + j] = (float)v[i][j];
+      if (ODD) o[C] = (float)rest;
+      trim(o, lane, d);
     }
   };
   template <typename S>
-  static __device__ __forceinline__ void store(S* p, const float (&v)[C], int lane, int d) {
+  static __device__ __forceinline__ void store(S* p, const float (&v)[N], int lane, int d) {
+    const int w = whole(d);
 #pragma unroll
     for (int i = 0; i < C / V; ++i) {
       const int c = col(i, lane);
-      if (c < d) store_run<S, V>(p + c, v + i * V);
+      if (c < w) store_run<S, V>(p + c, v + i * V);
     }
+    if (ODD && w + lane < d) p[w + lane] = (S)v[C];
   }
 };
 
@@ -136,30 +155,30 @@ __device__ __forceinline__ int seq_of(const int* off, int n, long long m) {
   return lo;
 }
 
-template <typename T, int L, int C, bool VEC>
+template <typename T, int L, int C, bool ODD>
 __global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_kernel(
     NormArgs a, const T* x, long long ldx, const T* b, long long ldb, T* r, long long ldr, T* n, long long ldn,
     long long run) {
-  using R = Row<T, L, C, VEC>;
+  using R = Row<T, L, C, ODD>;
   __shared__ float lds[L > 64 ? L / 64 * 8 : 1];
   int turn = 0;
   const int lane = threadIdx.x % L;
   const long long r0 = ((long long)blockIdx.x * R::kGroups + threadIdx.x / L) * run;
   const long long r1 = min(r0 + run, norm_limit(a));
-  float sw[C], wp[C], g[C];
+  float sw[R::N], wp[R::N], g[R::N];
 #pragma unroll
-  for (int j = 0; j < C; ++j) sw[j] = 1.f, wp[j] = 0.f, g[j] = 1.f;
+  for (int j = 0; j < R::N; ++j) sw[j] = 1.f, wp[j] = 0.f, g[j] = 1.f;
   if (a.scale) R::load(a.scale, sw, lane, a.d);
   if (a.w_post) {
-    float w[C];
+    float w[R::N];
     R::load(a.w_post, w, lane, a.d);
 #pragma unroll
-    for (int j = 0; j < C; ++j) sw[j] *= w[j];
+    for (int j = 0; j < R::N; ++j) sw[j] *= w[j];
   }
   if (a.w_pre) R::load(a.w_pre, wp, lane, a.d);
   long long seq_end = -1;
   for (long long m = r0; m < r1; ++m) {
-    float xv[C], bv[C];
+    float xv[R::N], bv[R::N];
     R::load(x + m * ldx, xv, lane, a.d);
     R::load(b + m * ldb, bv, lane, a.d);
     if (a.gate) {
@@ -176,13 +195,13 @@ __global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_kernel(
     if (a.w_post) {
       s[0] = 0.f;
 #pragma unroll
-      for (int j = 0; j < C; ++j) s[0] += bv[j] * bv[j];
+      for (int j = 0; j < R::N; ++j) s[0] += bv[j] * bv[j];
       group_sum<L, 1>(s, lds, turn);
       beta = 1.0f / sqrtf(s[0] * a.inv_d + a.eps);
     }
     s[0] = 0.f;
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
+    for (int j = 0; j < R::N; ++j) {
       xv[j] += bv[j] * beta * sw[j] * g[j];
       s[0] += xv[j] * xv[j];
     }
@@ -191,18 +210,18 @@ __global__ __launch_bounds__((L < 256 ? 256 : L)) void residual_norm_kernel(
       group_sum<L, 1>(s, lds, turn);
       const float rho = 1.0f / sqrtf(s[0] * a.inv_d + a.eps);
 #pragma unroll
-      for (int j = 0; j < C; ++j) xv[j] *= rho * wp[j];
+      for (int j = 0; j < R::N; ++j) xv[j] *= rho * wp[j];
       R::store(n + m * ldn, xv, lane, a.d);
     }
   }
 }
 
-template <typename T, int L, int C, bool VEC>
+template <typename T, int L, int C, bool ODD>
 __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residual_norm_grad_kernel(
     NormArgs a, const T* dr, long long lddr, const T* dn, long long lddn, const T* r, long long ldr, const T* b,
     long long ldb, T* dx, long long lddx, T* db, long long lddb, NormGradOut o, long long run) {
-  using R = Row<T, L, C, VEC>;
-  constexpr int kSum = R::kGroups > 1 ? R::kThreads * C : 1;
+  using R = Row<T, L, C, ODD>;
+  constexpr int kSum = R::kGroups > 1 ? R::kThreads * R::N : 1;
   __shared__ float lds[L > 64 ? L / 64 * 8 : 1];
   __shared__ float sums[kSum];
   int turn = 0;
@@ -210,15 +229,15 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residua
   const long long group = (long long)blockIdx.x * R::kGroups + threadIdx.x / L;
   const long long r0 = group * run;
   const long long r1 = min(r0 + run, norm_limit(a));
-  float sw[C], wp[C], g[C], P[C], Q[C], t[C];
+  float sw[R::N], wp[R::N], g[R::N], P[R::N], Q[R::N], t[R::N];
 #pragma unroll
-  for (int j = 0; j < C; ++j) sw[j] = 1.f, wp[j] = 0.f, g[j] = 1.f, P[j] = Q[j] = t[j] = 0.f;
+  for (int j = 0; j < R::N; ++j) sw[j] = 1.f, wp[j] = 0.f, g[j] = 1.f, P[j] = Q[j] = t[j] = 0.f;
   if (a.scale) R::load(a.scale, sw, lane, a.d);
   if (a.w_post) {
-    float w[C];
+    float w[R::N];
     R::load(a.w_post, w, lane, a.d);
 #pragma unroll
-    for (int j = 0; j < C; ++j) sw[j] *= w[j];
+    for (int j = 0; j < R::N; ++j) sw[j] *= w[j];
   }
   if (a.w_pre) R::load(a.w_pre, wp, lane, a.d);
   const T* gate = static_cast<const T*>(a.gate);
@@ -228,20 +247,22 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residua
   // the sequence's sum so far: whole, or the part that this run holds
   auto finish = [&](long long upto) {
 #pragma unroll
-    for (int j = 0; j < C; ++j) Q[j] += g[j] * t[j];
+    for (int j = 0; j < R::N; ++j) Q[j] += g[j] * t[j];
     if (dgate) {
       if (seq_begin >= r0 && seq_end <= upto) {
 #pragma unroll
-        for (int j = 0; j < C; ++j) t[j] *= sw[j];
+        for (int j = 0; j < R::N; ++j) t[j] *= sw[j];
         R::store(dgate + seq * o.lddg, t, lane, a.d);
       } else {
         R::store(o.part_seq + (2 * group + (seq_begin >= r0)) * a.d, t, lane, a.d);
       }
     }
 #pragma unroll
-    for (int j = 0; j < C; ++j) t[j] = 0.f;
+    for (int j = 0; j < R::N; ++j) t[j] = 0.f;
   };
-  typename R::Raw ahead_b, ahead_dr, ahead_r, ahead_dn;   // the next row, where there are registers for it
+  // the next row, where there are registers for it
+  constexpr bool kAhead = !ODD && (C == 8 || sizeof(T) == 2);
+  typename R::Raw ahead_b, ahead_dr, ahead_r, ahead_dn;
   auto fetch = [&](long long m) {
     ahead_b.load(b + m * ldb, lane, a.d);
     if (dr) ahead_dr.load(dr + m * lddr, lane, a.d);
@@ -250,23 +271,27 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residua
       ahead_dn.load(dn + m * lddn, lane, a.d);
     }
   };
-  constexpr bool kAhead = C == 8 || sizeof(T) == 2;
   if (kAhead && r0 < r1) fetch(r0);
   for (long long m = r0; m < r1; ++m) {
-    float D[C], bv[C], rv[C], nv[C];
-    if (!kAhead) fetch(m);
-    ahead_b.values(bv, lane, a.d);
-    if (dr) {
-      ahead_dr.values(D, lane, a.d);
-    } else {
+    float D[R::N], bv[R::N], rv[R::N], nv[R::N];
 #pragma unroll
-      for (int j = 0; j < C; ++j) D[j] = 0.f;
+    for (int j = 0; j < R::N; ++j) D[j] = 0.f;
+    if constexpr (kAhead) {
+      ahead_b.values(bv, lane, a.d);
+      if (dr) ahead_dr.values(D, lane, a.d);
+      if (a.w_pre) {
+        ahead_r.values(rv, lane, a.d);
+        ahead_dn.values(nv, lane, a.d);
+      }
+      if (m + 1 < r1) fetch(m + 1);
+    } else {
+      R::load(b + m * ldb, bv, lane, a.d);
+      if (dr) R::load(dr + m * lddr, D, lane, a.d);
+      if (a.w_pre) {
+        R::load(r + m * ldr, rv, lane, a.d);
+        R::load(dn + m * lddn, nv, lane, a.d);
+      }
     }
-    if (a.w_pre) {
-      ahead_r.values(rv, lane, a.d);
-      ahead_dn.values(nv, lane, a.d);
-    }
-    if (kAhead && m + 1 < r1) fetch(m + 1);
     if (a.gate) {
       if (!a.gate_off) {
         R::load(gate + m * a.ldg, g, lane, a.d);
@@ -281,18 +306,18 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residua
     float s[3] = {0.f, 0.f, 0.f};
     if (a.w_pre) {
 #pragma unroll
-      for (int j = 0; j < C; ++j) s[0] += rv[j] * rv[j], s[1] += wp[j] * nv[j] * rv[j];
+      for (int j = 0; j < R::N; ++j) s[0] += rv[j] * rv[j], s[1] += wp[j] * nv[j] * rv[j];
     }
     if (a.w_post) {
 #pragma unroll
-      for (int j = 0; j < C; ++j) s[2] += bv[j] * bv[j];
+      for (int j = 0; j < R::N; ++j) s[2] += bv[j] * bv[j];
     }
     if (a.w_pre || a.w_post) group_sum<L, 3>(s, lds, turn);
     if (a.w_pre) {
       const float rho = 1.0f / sqrtf(s[0] * a.inv_d + a.eps);
       const float k = rho * rho * (s[1] * a.inv_d);
 #pragma unroll
-      for (int j = 0; j < C; ++j) {
+      for (int j = 0; j < R::N; ++j) {
         const float rh = rv[j] * rho;
         D[j] += rho * wp[j] * nv[j] - rh * k;
         P[j] += nv[j] * rh;
@@ -304,13 +329,13 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residua
       beta = 1.0f / sqrtf(s[2] * a.inv_d + a.eps);
       float q[1] = {0.f};
 #pragma unroll
-      for (int j = 0; j < C; ++j) q[0] += D[j] * sw[j] * g[j] * bv[j];
+      for (int j = 0; j < R::N; ++j) q[0] += D[j] * sw[j] * g[j] * bv[j];
       group_sum<L, 1>(q, lds, turn);
       k = beta * beta * (q[0] * a.inv_d);
     }
-    float e[C];
+    float e[R::N];
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
+    for (int j = 0; j < R::N; ++j) {
       const float bh = bv[j] * beta, Tj = D[j] * bh;
       e[j] = beta * (D[j] * sw[j] * g[j]) - bh * k;
       if (a.gate_off) {
@@ -325,18 +350,18 @@ __global__ __launch_bounds__((L < 256 ? 256 : L), (C == 8 ? 3 : 2)) void residua
   }
   if (seq >= 0) finish(r1);
   // the workgroup's groups, added in order
-  auto join = [&](float (&v)[C], float* out) {
+  auto join = [&](float (&v)[R::N], float* out) {
     if constexpr (R::kGroups == 1) {
       R::store(out, v, lane, a.d);
     } else {
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < C; ++j) sums[j * R::kThreads + threadIdx.x] = v[j];
+      for (int j = 0; j < R::N; ++j) sums[j * R::kThreads + threadIdx.x] = v[j];
       __syncthreads();
       if (threadIdx.x < L) {
         for (int q = 1; q < R::kGroups; ++q) {
 #pragma unroll
-          for (int j = 0; j < C; ++j) v[j] += sums[j * R::kThreads + q * L + lane];
+          for (int j = 0; j < R::N; ++j) v[j] += sums[j * R::kThreads + q * L + lane];
         }
         R::store(out, v, lane, a.d);
       }
@@ -362,10 +387,10 @@ __device__ __forceinline__ float sum_apart(const float* p, long long stride, int
 }
 
 // Adds the partials.  Workgroups with blockIdx.y = 0 (dw_pre) and 1 (Q) own 16 columns; 32 slices of consecutive
-// partials are added in order.  The others own sequences whose rows lie in several runs, and clear the gradients
-// of sequences without rows.
+// partials are added in order.  The others own SCOLS columns of sequences whose rows lie in several runs (in
+// slices, like those), and clear the gradients of sequences without rows.
 constexpr int kFinishSlices = 32;
-template <typename T>
+template <typename T, int SCOLS>
 __global__ __launch_bounds__(16 * kFinishSlices) void residual_norm_finish_kernel(NormArgs a, NormGradOut o, int parts,
                                                                                   long long run, float* dw_post,
                                                                                   float* dscale, float* dw_pre) {
@@ -395,20 +420,32 @@ __global__ __launch_bounds__(16 * kFinishSlices) void residual_norm_finish_kerne
   }
   T* dgate = static_cast<T*>(o.dgate);
   const long long limit = norm_limit(a);
-  for (int s = blockIdx.x + gridDim.x * (blockIdx.y - 2); s < a.n_seq; s += gridDim.x * (gridDim.y - 2)) {
+  constexpr int kSlices = 16 * kFinishSlices / SCOLS;
+  __shared__ float red[kSlices][SCOLS];
+  const int cl = threadIdx.x % SCOLS, sl = threadIdx.x / SCOLS, tiles = (a.d + SCOLS - 1) / SCOLS;
+  const long long blocks = (long long)gridDim.x * (gridDim.y - 2);
+  for (long long i = blockIdx.x + (long long)gridDim.x * (blockIdx.y - 2); i < (long long)a.n_seq * tiles; i += blocks) {
+    const long long s = i / tiles;
+    const int c = (int)(i % tiles) * SCOLS + cl;
     const long long m0 = max((long long)a.gate_off[s], 0ll), m1 = min((long long)a.gate_off[s + 1], limit);
     const bool empty = m1 <= m0;
     const long long w0 = empty ? 0 : m0 / run, w1 = empty ? 0 : (m1 - 1) / run;
     if (!empty && w0 == w1) continue;   // its run has written it
-    for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
-      float v = 0.f;
-      if (!empty) {
-        v = o.part_seq[(2 * w0 + 1) * a.d + c] + sum_apart(o.part_seq + 2 * (w0 + 1) * a.d + c, 2ll * a.d, (int)(w1 - w0));
-        if (a.scale) v *= a.scale[c];
-        if (a.w_post) v *= a.w_post[c];
-      }
+    const long long each = (w1 - w0 + kSlices - 1) / kSlices, q0 = sl * each;   // of the parts behind the first
+    float v = 0.f;
+    if (c < a.d && q0 < w1 - w0)
+      v = sum_apart(o.part_seq + 2 * (w0 + 1 + q0) * a.d + c, 2ll * a.d, (int)min(each, w1 - w0 - q0));
+    red[sl][cl] = v;
+    __syncthreads();
+    if (sl == 0 && c < a.d) {
+      v = empty ? 0.f : o.part_seq[(2 * w0 + 1) * a.d + c];
+#pragma unroll
+      for (int q = 0; q < kSlices; ++q) v += red[q][cl];
+      if (a.scale) v *= a.scale[c];
+      if (a.w_post) v *= a.w_post[c];
       dgate[s * o.lddg + c] = (T)v;
     }
+    __syncthreads();
   }
 }
 
@@ -465,14 +502,6 @@ static NormArgs norm_args(const janus_norm* p) {
                   p->d, p->gate_off ? p->n_seq : 0, p->eps, 1.0f / (float)p->d};
 }
 
-// Whether the 16-byte accesses may be used: every row and parameter starts on 16 bytes and the width is
-// whole runs.
-static bool norm_vec(const janus_norm* p) {
-  const int e = type_bytes(p->type);
-  return p->d % (16 / e) == 0 && rows_aligned(p->gate, p->ldg, e) && rows_aligned(p->w_post, 0, 4) &&
-         rows_aligned(p->scale, 0, 4) && rows_aligned(p->w_pre, 0, 4);
-}
-
 }  // namespace janus
 
 using namespace janus;
@@ -484,22 +513,20 @@ extern "C" int janus_residual_norm(const janus_norm* p, const void* x, int64_t l
   if (p->rows > 0 && (!x || !b || !r || ldx < p->d || ldb < p->d || ldr < p->d)) return JANUS_EINVAL;
   if (p->rows > 0 && ((p->w_pre && (!n || ldn < p->d)) || (!p->w_pre && n))) return JANUS_EINVAL;
   if (p->rows == 0) return JANUS_OK;
-  const int e = type_bytes(p->type);
-  const bool vec = norm_vec(p) && rows_aligned(x, ldx, e) && rows_aligned(b, ldb, e) && rows_aligned(r, ldr, e) &&
-                   rows_aligned(n, ldn, e);
+  const bool odd = p->d % (16 / type_bytes(p->type)) != 0;
   const NormArgs a = norm_args(p);
   const NormPlan plan = norm_plan(p->rows, p->d, kForwardBlocks);
   with_type(p->type, [&](auto zero) {
     using T = decltype(zero);
     with_shape(p->d, [&](auto L, auto C) {
-      auto go = [&](auto V) {
-        constexpr bool kVec = decltype(V)::value;
-        using R = Row<T, L.value, C.value, kVec>;
-        hipLaunchKernelGGL((residual_norm_kernel<T, L.value, C.value, kVec>), dim3(plan.blocks), dim3(R::kThreads), 0,
+      auto go = [&](auto rest) {
+        constexpr bool kOdd = decltype(rest)::value;
+        using R = Row<T, L.value, C.value, kOdd>;
+        hipLaunchKernelGGL((residual_norm_kernel<T, L.value, C.value, kOdd>), dim3(plan.blocks), dim3(R::kThreads), 0,
                            static_cast<hipStream_t>(stream), a, static_cast<const T*>(x), ldx,
                            static_cast<const T*>(b), ldb, static_cast<T*>(r), ldr, static_cast<T*>(n), ldn, plan.run);
       };
-      if (vec) go(std::true_type{});
+      if (odd) go(std::true_type{});
       else go(std::false_type{});
     });
   });
@@ -529,11 +556,7 @@ extern "C" int janus_residual_norm_grad(const janus_norm* p, const void* dr, int
     return JANUS_EINVAL;
   if (!work || reinterpret_cast<uintptr_t>(work) % 16 || work_bytes < janus_residual_norm_grad_workspace(p))
     return JANUS_EINVAL;
-  const int e = type_bytes(p->type);
-  // the partials are rows of d floats, so d is whole runs of 16 bytes of those too
-  const bool vec = norm_vec(p) && rows_aligned(dr, lddr, e) && rows_aligned(dn, lddn, e) && rows_aligned(r, ldr, e) &&
-                   rows_aligned(b, ldb, e) && rows_aligned(dx, lddx, e) && rows_aligned(db, lddb, e) &&
-                   rows_aligned(dgate, lddg, e);
+  const bool odd = p->d % (16 / type_bytes(p->type)) != 0;
   const NormArgs a = norm_args(p);
   const NormPlan plan = norm_plan(p->rows, p->d, grad_blocks(p->d));
   NormGradOut o{static_cast<float*>(work), nullptr, dgate, lddg};
@@ -543,23 +566,30 @@ extern "C" int janus_residual_norm_grad(const janus_norm* p, const void* dr, int
     using T = decltype(zero);
     if (plan.blocks > 0)
       with_shape(p->d, [&](auto L, auto C) {
-        auto go = [&](auto V) {
-          constexpr bool kVec = decltype(V)::value;
-          using R = Row<T, L.value, C.value, kVec>;
-          hipLaunchKernelGGL((residual_norm_grad_kernel<T, L.value, C.value, kVec>), dim3(plan.blocks),
+        auto go = [&](auto rest) {
+          constexpr bool kOdd = decltype(rest)::value;
+          using R = Row<T, L.value, C.value, kOdd>;
+          hipLaunchKernelGGL((residual_norm_grad_kernel<T, L.value, C.value, kOdd>), dim3(plan.blocks),
                              dim3(R::kThreads), 0, st, a, static_cast<const T*>(dr), lddr, static_cast<const T*>(dn),
                              lddn, static_cast<const T*>(r), ldr, static_cast<const T*>(b), ldb, static_cast<T*>(dx),
                              lddx, static_cast<T*>(db), lddb, o, plan.run);
         };
-        if (vec) go(std::true_type{});
+        if (odd) go(std::true_type{});
         else go(std::false_type{});
       });
     const bool sums = dw_post || dscale || dw_pre, seqs = dgate && a.gate_off && a.n_seq > 0;
     if (sums || seqs) {
-      const int bx = (int)cdiv(p->d, 16);
-      const int by = seqs ? 2 + (int)cdiv(a.n_seq < 2048 ? a.n_seq : 2048, bx) : 2;
-      hipLaunchKernelGGL(residual_norm_finish_kernel<T>, dim3(bx, by), dim3(16 * kFinishSlices), 0, st, a, o, plan.blocks,
-                         plan.run, dw_post, dscale, dw_pre);
+      const unsigned bx = cdiv(p->d, 16);
+      auto finish = [&](auto cols) {
+        const long long blocks = seqs ? (long long)a.n_seq * cdiv(p->d, cols.value) : 0;
+        hipLaunchKernelGGL((residual_norm_finish_kernel<T, cols.value>),
+                           dim3(bx, 2 + cdiv(blocks < 8192 ? blocks : 8192, bx)), dim3(16 * kFinishSlices), 0, st, a, o,
+                           plan.blocks, plan.run, dw_post, dscale, dw_pre);
+      };
+      // many short sequences: few slices of many columns; few long ones: the other way round
+      const long long runs = (long long)plan.blocks * plan.groups_per_block;
+      if (runs <= 16ll * a.n_seq) finish(std::integral_constant<int, 128>{});
+      else finish(std::integral_constant<int, 16>{});
     }
   });
   return launched();

@@ -21,10 +21,10 @@ __device__ __forceinline__ int pack_code(float top) {
 // 2^(c - 127), NaN for 255
 __device__ __forceinline__ float code_scale(int c) { return __int_as_float(c == 255 ? 0x7FC00000 : c << 23); }
 
-// Eight columns of a row from column c, zero past d.  `wide`: the row's addresses allow whole runs.
+// Eight columns of a row from column c, zero past d.
 template <typename T>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int c, int d, bool wide, float (&v)[8]) {
-  if (wide && c + 8 <= d) {
+__device__ __forceinline__ void load8(const T* __restrict__ row, int c, int d, float (&v)[8]) {
+  if (c + 8 <= d) {
     load_run<T, 8>(row + c, v);
   } else {
 #pragma unroll
@@ -32,8 +32,8 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, int c, int d, b
   }
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* __restrict__ row, int c, int d, bool wide, const float (&v)[8]) {
-  if (wide && c + 8 <= d) {
+__device__ __forceinline__ void store8(T* __restrict__ row, int c, int d, const float (&v)[8]) {
+  if (c + 8 <= d) {
     store_run<T, 8>(row + c, v);
   } else {
 #pragma unroll
@@ -41,26 +41,13 @@ __device__ __forceinline__ void store8(T* __restrict__ row, int c, int d, bool w
       if (c + j < d) row[c + j] = (T)v[j];
   }
 }
-__device__ __forceinline__ void load8q(const int8_t* __restrict__ row, int c, int d, bool wide, float (&v)[8]) {
-  if (wide && c + 8 <= d) {
-    const uint2 u = *reinterpret_cast<const uint2*>(row + c);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = (float)(int8_t)(u.x >> (8 * j));
-      v[4 + j] = (float)(int8_t)(u.y >> (8 * j));
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? (float)row[c + j] : 0.f;
-  }
-}
+typedef unsigned bytes8 __attribute__((ext_vector_type(2), aligned(1)));
 
 // Rows are shared out over `tpr` threads (a power of two, at most 256) of eight columns each; four
 // neighbouring threads hold a block.
 struct PackShape {
   long long rows;
   int d, tpr;
-  bool wide_x, wide_q, wide_g, wide_v;
 };
 
 template <typename T>
@@ -72,7 +59,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackShape s, const T* __
   for (long long m = (long long)blockIdx.x * per + threadIdx.x / s.tpr; m < s.rows; m += (long long)gridDim.x * per) {
     for (int c = t * 8; c < cols; c += s.tpr * 8) {
       float v[8], top = 0.f;
-      load8(x + m * ldx, c, s.d, s.wide_x, v);
+      load8(x + m * ldx, c, s.d, v);
       int bad = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -91,8 +78,8 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackShape s, const T* __
         w[j >> 2] |= (unsigned)(n & 255) << (8 * (j & 3));
       }
       int8_t* out = q + m * ldq + c;
-      if (s.wide_q && c + 8 <= s.d) {
-        *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+      if (c + 8 <= s.d) {
+        *reinterpret_cast<bytes8*>(out) = bytes8{w[0], w[1]};
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -113,22 +100,22 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
   for (long long m = (long long)blockIdx.x * per + threadIdx.x / s.tpr; m < s.rows; m += (long long)gridDim.x * per) {
     for (int c = t * 8; c < s.d; c += s.tpr * 8) {
       float v[8];
-      load8q(q + m * ldq, c, s.d, s.wide_q, v);
+      load8(q + m * ldq, c, s.d, v);
       const float scale = code_scale(code[m * ldc + c / kPackBlock]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= scale;
       if constexpr (kSilu) {
         if (out) {
           float g[8];
-          load8(grad + m * ldg, c, s.d, s.wide_g, g);
+          load8(grad + m * ldg, c, s.d, g);
 #pragma unroll
           for (int j = 0; j < 8; ++j) g[j] *= silu_d1(v[j]);
-          store8(out + m * ldo, c, s.d, s.wide_x, g);
+          store8(out + m * ldo, c, s.d, g);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = silu(v[j]);
       }
-      if (value) store8(value + m * ldv, c, s.d, s.wide_v, v);
+      if (value) store8(value + m * ldv, c, s.d, v);
     }
   }
 }
@@ -175,34 +162,35 @@ __device__ __forceinline__ unsigned pack_high(float a, float b) {   // the upper
 }
 __device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
 
-// Rows of a chunk as a buffer: reads behind its last value give zero, so a chunk's ragged end needs no code.
+// Where the rows of both operands start on 16 bytes (WIDE), a chunk's rows are a buffer: reads behind its last
+// value give zero, so its ragged end needs no code.  Other rows are read by runs at any address, up to the last
+// whole one, and value by value from there; rows behind the chunk are skipped.
 typedef __amdgpu_buffer_rsrc_t buffer;
 __device__ __forceinline__ buffer rows_buffer(const void* p, unsigned bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-// Eight values of a row of B at byte `at`, and their planes.
+// Eight values of a row of B, and their planes.
 template <typename T>
 struct Octet {
   T v[8];
-  template <bool WIDE>
   __device__ __forceinline__ void load(buffer b, unsigned at) {
-    if constexpr (WIDE) {
-      typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
-      constexpr int V = 16 / (int)sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+    constexpr int V = 16 / (int)sizeof(T);
 #pragma unroll
-      for (int j = 0; j < 8; j += V) {
-        const vec u = __builtin_bit_cast(vec, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at + j * sizeof(T), 0, 0));
+    for (int j = 0; j < 8; j += V) {
+      const vec u = __builtin_bit_cast(vec, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at + j * sizeof(T), 0, 0));
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j + i] = u[i];
-      }
+      for (int i = 0; i < V; ++i) v[j + i] = u[i];
+    }
+  }
+  __device__ __forceinline__ void load(const T* __restrict__ row, int c, int n) {   // n = 0: no row
+    if (c + 8 <= n) {
+      __builtin_memcpy(v, row + c, sizeof v);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (sizeof(T) == 4) v[j] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(b, at + 4 * j, 0, 0));
-        else v[j] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(b, at + 2 * j, 0, 0));
-      }
+      for (int j = 0; j < 8; ++j) v[j] = c + j < n ? row[c + j] : (T)0.f;
     }
   }
   __device__ __forceinline__ void planes(uint4 (&o)[Terms<T>::kPlanes]) const {
@@ -230,17 +218,20 @@ struct Octet {
 struct Sixteen {
   u32x4 q;
   int code;
-  template <bool WIDE>
   __device__ __forceinline__ void load(buffer b, unsigned at, buffer codes, unsigned at_code) {
-    if constexpr (WIDE) {
-      q = (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0);
+    q = (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0);
+    code = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(codes, at_code, 0, 0);
+  }
+  __device__ __forceinline__ void load(const int8_t* __restrict__ row, const uint8_t* __restrict__ codes, int c, int n) {
+    if (c + 16 <= n) {
+      __builtin_memcpy(&q, row + c, 16);
     } else {
       q = u32x4{};
 #pragma unroll
       for (int j = 0; j < 16; ++j)
-        q[j >> 2] |= (unsigned)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(b, at + j, 0, 0) << (8 * (j & 3));
+        if (c + j < n) q[j >> 2] |= (unsigned)(uint8_t)row[c + j] << (8 * (j & 3));
     }
-    code = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(codes, at_code, 0, 0);
+    code = c < n ? codes[c / kPackBlock] : 0;
   }
   // the half `first` of them, then the other
   __device__ __forceinline__ void values(int first, uint4 (&o)[2]) const {
@@ -271,11 +262,10 @@ __device__ __forceinline__ bf16x8 read_columns(const char* lo, const char* hi) {
 // Where a row's 32-byte unit lies.
 __device__ __forceinline__ int place(int unit, int m) { return unit ^ (2 * (m & 3)); }
 
-// Bytes of `rows` rows up to the last one's last value; where they are read by 16 bytes, rounded up to those.
-template <bool WIDE>
-__device__ __forceinline__ unsigned last_byte(int rows, long long ld, int width, int size) {
+// Bytes of `rows` rows up to the last one's last value, rounded up to the `unit` by which they are read.
+__device__ __forceinline__ unsigned last_byte(int rows, long long ld, int width, int size, unsigned unit) {
   const unsigned n = rows ? (unsigned)(((rows - 1) * ld + width) * size) : 0u;
-  return WIDE ? (n + 15) & ~15u : n;
+  return (n + unit - 1) & ~(unit - 1);
 }
 
 template <typename T, bool WIDE>
@@ -301,9 +291,9 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
 
   // staging: thread t holds 16 values of X's row t / 8 and, per pass, 8 values of a row of B
   const int rows = ch.r1 - ch.r0;
-  const buffer bufA = rows_buffer(q + ch.r0 * ldq, last_byte<WIDE>(rows, ldq, P, 1));
-  const buffer bufC = rows_buffer(code + ch.r0 * ldc, last_byte<false>(rows, ldc, (P + kPackBlock - 1) / kPackBlock, 1));
-  const buffer bufB = rows_buffer(b + ch.r0 * ldb, last_byte<WIDE>(rows, ldb, Q, sizeof(T)));
+  const buffer bufA = rows_buffer(q + ch.r0 * ldq, last_byte(rows, ldq, P, 1, 16));
+  const buffer bufC = rows_buffer(code + ch.r0 * ldc, last_byte(rows, ldc, (P + kPackBlock - 1) / kPackBlock, 1, 1));
+  const buffer bufB = rows_buffer(b + ch.r0 * ldb, last_byte(rows, ldb, Q, sizeof(T), 16));
   const int ma = t >> 3, ua = t & 7, half = ma & 1;
   const int wa = ma * kRowA + (place(ua, ma) << 5);
   constexpr int kPerRow = COLS / 8, kRowsPass = 256 / kPerRow;
@@ -315,13 +305,25 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
     Sixteen a;
     Octet<T> b[kPass];
   };
-  auto load = [&](Regs& r) {   // the next stage's values
-    r.a.template load<WIDE>(bufA, atA, bufC, atC);
+  int ahead = ch.r0;   // the next stage's first row
+  auto load = [&](Regs& r) {
+    if constexpr (WIDE) {
+      r.a.load(bufA, atA, bufC, atC);
 #pragma unroll
-    for (int i = 0; i < kPass; ++i) r.b[i].template load<WIDE>(bufB, atB + i * passB);
-    atA += kWgRows * (unsigned)ldq;
-    atC += kWgRows * (unsigned)ldc;
-    atB += stepB;
+      for (int i = 0; i < kPass; ++i) r.b[i].load(bufB, atB + i * passB);
+      atA += kWgRows * (unsigned)ldq;
+      atC += kWgRows * (unsigned)ldc;
+      atB += stepB;
+    } else {
+      const long long ra = ahead + ma;
+      r.a.load(q + ra * ldq, code + ra * ldc, p0 + 16 * ua, ra < ch.r1 ? P : 0);
+#pragma unroll
+      for (int i = 0; i < kPass; ++i) {
+        const long long rb = ahead + mb + i * kRowsPass;
+        r.b[i].load(b + rb * ldb, c0 + 8 * ob, rb < ch.r1 ? Q : 0);
+      }
+      ahead += kWgRows;
+    }
   };
   auto stage = [&](const Regs& r, char* to) {
     uint4 o[2];   // odd rows write their second half first: two rows then fill all banks
@@ -497,7 +499,7 @@ static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
 static PackShape pack_shape(long long rows, int d) {
   int tpr = 4;
   while (tpr < 256 && tpr * 8 < d) tpr <<= 1;
-  return PackShape{rows, d, tpr, false, false, false, false};
+  return PackShape{rows, d, tpr};
 }
 static unsigned pack_grid(const PackShape& s) {
   const long long need = (s.rows + 256 / s.tpr - 1) / (256 / s.tpr);
@@ -520,9 +522,7 @@ extern "C" int janus_pack_rows(const void* x, int64_t ldx, int32_t type, int64_t
   if (rc) return rc;
   if (rows > 0 && (!x || ldx < d)) return JANUS_EINVAL;
   if (rows == 0) return JANUS_OK;
-  PackShape s = pack_shape(rows, d);
-  s.wide_x = rows_aligned(x, ldx, type_bytes(type));
-  s.wide_q = rows_aligned(q, ldq, 1, 8);
+  const PackShape s = pack_shape(rows, d);
   with_type(type, [&](auto zero) {
     using T = decltype(zero);
     hipLaunchKernelGGL(pack_rows_kernel<T>, dim3(pack_grid(s)), dim3(256), 0, static_cast<hipStream_t>(stream), s,
@@ -541,12 +541,7 @@ extern "C" int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* co
   if ((!grad) != (!out) || (act == JANUS_ACT_NONE && grad) || (!out && !value) || (grad && (ldg < d || ldo < d)) ||
       (value && ldv < d))
     return JANUS_EINVAL;
-  const int e = type_bytes(type);
-  PackShape s = pack_shape(rows, d);
-  s.wide_q = rows_aligned(q, ldq, 1, 8);
-  s.wide_g = rows_aligned(grad, ldg, e);
-  s.wide_x = rows_aligned(out, ldo, e);
-  s.wide_v = rows_aligned(value, ldv, e);
+  const PackShape s = pack_shape(rows, d);
   with_type(type, [&](auto zero) {
     using T = decltype(zero);
     auto go = [&](auto silu) {

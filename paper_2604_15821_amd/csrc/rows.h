@@ -13,15 +13,15 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// N consecutive values as fp32.  The address is a multiple of their size, at most of 16 bytes.
-// Stores round to nearest, ties to even.
+// N consecutive values as fp32, in pieces of at most 16 bytes, at any multiple of their size (the memory
+// takes runs at any address; ones that cross a line cost a second access).  Stores round to nearest, ties to
+// even.
 template <typename T, int N>
 __device__ __forceinline__ void load_run(const T* __restrict__ p, float* v) {
-  constexpr int kBytes = sizeof(T) * N;
-  typedef T vec __attribute__((ext_vector_type(N)));
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
   if constexpr (N == 1) {
     v[0] = (float)p[0];
-  } else if constexpr (kBytes <= 16) {
+  } else if constexpr (sizeof(T) * N <= 16) {
     const vec u = *reinterpret_cast<const vec*>(p);
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = (float)u[j];
@@ -32,11 +32,10 @@ __device__ __forceinline__ void load_run(const T* __restrict__ p, float* v) {
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_run(T* __restrict__ p, const float* v) {
-  constexpr int kBytes = sizeof(T) * N;
-  typedef T vec __attribute__((ext_vector_type(N)));
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
   if constexpr (N == 1) {
     p[0] = (T)v[0];
-  } else if constexpr (kBytes <= 16) {
+  } else if constexpr (sizeof(T) * N <= 16) {
     vec u;
 #pragma unroll
     for (int j = 0; j < N; ++j) u[j] = (T)v[j];
