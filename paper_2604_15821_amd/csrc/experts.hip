@@ -19,10 +19,10 @@ struct ExpertArgs {
   const float* beta;
 };
 
-// Router of one token by a workgroup of W waves.  Lanes take V neighbouring experts each (four where rows of the
-// router start on 16 bytes), the rest of a wave and the waves take rows, eight in flight; rows are added over
-// the lanes and then over the waves.  Every expert then counts those that come before it: its rank is its
-// place among the chosen, without a round for each of them.
+// Router of one token by a workgroup of W waves.  Lanes take V neighbouring experts each (four, of which the last
+// lane's may be its neighbour's too; one where there are fewer), the rest of a wave and the waves take rows, up to
+// sixteen in flight; rows are added over the lanes and then over the waves.  Every expert then counts
+// those that come before it: its rank is its place among the chosen, without a round for each of them.
 // NaN ranks like -inf and makes the token's gates NaN; a token without any finite or +inf logit
 // (all experts masked) has gates of zero.
 template <int W>
@@ -34,35 +34,43 @@ struct RouteArea {
 };
 template <typename T, int V, int W>
 __device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __restrict__ x, RouteArea<W>& s) {
-  typedef float vec __attribute__((ext_vector_type(V)));
+  typedef float vec __attribute__((ext_vector_type(V), aligned(4)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int kFlight = 8;
   const int units = (a.n + V - 1) / V;
   int wide = 1;
   while (wide < units && wide < 64) wide <<= 1;
   const int per = 64 / wide, rows = per * W, row0 = wave * per + lane / wide;
   if (threadIdx.x == 0) s.nan = 0;
   for (int u0 = 0; u0 < units; u0 += 64) {
-    const int u = u0 + (lane & (wide - 1));
+    const int u = u0 + (lane & (wide - 1)), c0 = max(min(V * u, a.n - V), 0);
     vec sum = {};
-    const float* w = a.router + V * min(u, units - 1);
-    for (int i = row0; i < a.d; i += kFlight * rows) {
-      vec r[kFlight];
-      float v[kFlight];
+    const float* w = a.router + c0;
+    auto add = [&](auto flight, int i) {   // rows i, i + rows, ..; past the end the last one is read and not added
+      vec r[flight.value];
+      float v[flight.value];
 #pragma unroll
-      for (int j = 0; j < kFlight; ++j) {
+      for (int j = 0; j < flight.value; ++j) {
         const int q = min(i + j * rows, a.d - 1);
         r[j] = *reinterpret_cast<const vec*>(w + (long long)q * a.n);
         v[j] = (float)x[q];
       }
 #pragma unroll
-      for (int j = 0; j < kFlight; ++j)
+      for (int j = 0; j < flight.value; ++j)
         if (i + j * rows < a.d) sum += r[j] * v[j];
+    };
+    for (int i = 0; i < a.d;) {
+      if (i + 8 * rows < a.d) {
+        add(std::integral_constant<int, 16>{}, i + row0);
+        i += 16 * rows;
+      } else {
+        add(std::integral_constant<int, 8>{}, i + row0);
+        i += 8 * rows;
+      }
     }
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       for (int o = wide; o < 64; o <<= 1) sum[c] += __shfl_xor(sum[c], o, 64);
-      if (lane < wide && u < units) s.red[wave][V * u + c] = sum[c];
+      if (lane < wide && u < units) s.red[wave][c0 + c] = sum[c];
     }
   }
   __syncthreads();
@@ -270,21 +278,21 @@ __device__ __forceinline__ int find_slots(const ExpertArgs& a, const int* __rest
   return s.count;
 }
 
-// One expert's tokens times COLS * 16 columns of its weight, over the rows [k0, k1) of it; the waves take stages
-// of 32 rows in turn and are added in order.  done(t, c, v): value of the t-th slot in column c.
+// One expert's slots base .. base + 16 MT - 1 times COLS * 16 columns of its weight, over the rows [k0, k1) of it; the
+// waves take stages of 32 rows in turn and are added in order.  done(t, c, v): value of the t-th slot in column c.
 // `A` is the operand of a token's values S, row ld apart, slot q reading row q / per.
 template <typename T, typename S, typename A, int COLS, int MT, typename F>
-__device__ __forceinline__ void expert_product(const ExpertSlots& s, const S* __restrict__ x, long long ldx, int per,
+__device__ __forceinline__ void expert_product(const ExpertSlots& s, int base, const S* __restrict__ x, long long ldx, int per,
                                                const T* __restrict__ w, int n, int k0, int k1, int K,
                                                float* __restrict__ lds, F done) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = 8 * (lane >> 4);
   const int c0 = blockIdx.x * (16 * COLS);
   // columns past the end (n is a multiple of 16, so of COLS) read the last ones and are not stored
   const T* wl = w + min(c0 + COLS * (lane & 15), n - COLS);
-  const int tiles = (s.count + 15) >> 4;
+  const int count = min(s.count - base, 16 * MT), tiles = (count + 15) >> 4;
   const S* xr[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) xr[m] = x + s.slot[min(16 * m + (lane & 15), s.count - 1)] / per * ldx;
+  for (int m = 0; m < MT; ++m) xr[m] = x + s.slot[base + min(16 * m + (lane & 15), count - 1)] / per * ldx;
   f32x4 acc[MT][COLS];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -322,13 +330,13 @@ __device__ __forceinline__ void expert_product(const ExpertSlots& s, const S* __
         }
     }
     __syncthreads();
-    const int rows = min(16, s.count - 16 * m);
+    const int rows = min(16, count - 16 * m);
     for (int e = threadIdx.x; e < rows * 16 * COLS; e += 64 * kExpertWaves) {
       float v = 0.f;
 #pragma unroll
       for (int q = 0; q < kExpertWaves; ++q) v += lds[q * (256 * COLS) + e];
       const int c = c0 + e % (16 * COLS);
-      if (c < n) done(16 * m + e / (16 * COLS), c, v);
+      if (c < n) done(base + 16 * m + e / (16 * COLS), c, v);
     }
   }
 }
@@ -356,7 +364,8 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs
   } else {
     if (find_slots(a, eid, s) == 0) return;
   }
-  expert_product<T, T, Eight<T>, COLS, MT>(s, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d, a.d, lds,
+  for (int base = 0; base < s.count; base += 16 * MT)
+    expert_product<T, T, Eight<T>, COLS, MT>(s, base, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d, a.d, lds,
                                            [&](int t, int c, float v) {
                                              hidden[(long long)s.slot[t] * a.h + c] = silu(v);
                                            });
@@ -401,8 +410,9 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_down_kernel(ExpertAr
   __shared__ float lds[kExpertWaves * 256 * COLS];
   __shared__ int last;
   const int splits = gridDim.z, k0 = blockIdx.z * rows_per_split;
-  if (find_slots(a, eid, s) > 0)
-    expert_product<T, float, A, COLS, MT>(s, hidden, a.h, 1, w2 + (long long)s.expert * a.h * a.d, a.d, k0,
+  const int count = find_slots(a, eid, s);
+  for (int base = 0; base < count; base += 16 * MT)
+    expert_product<T, float, A, COLS, MT>(s, base, hidden, a.h, 1, w2 + (long long)s.expert * a.h * a.d, a.d, k0,
                                           min(k0 + rows_per_split, a.h), a.h, lds, [&](int t, int c, float v) {
                                             float* o = part + ((long long)s.slot[t] * splits + blockIdx.z) * a.d + c;
                                             if constexpr (kJoin)
@@ -434,7 +444,9 @@ __global__ __launch_bounds__(256) void expert_join_kernel(ExpertArgs a, const fl
   if (c < a.d) y[t * ldy + c] = (T)expert_sum(a, gate, part, splits, t, c, [](float* p) { return *p; });
 }
 
-// How a call is shared out.  A workgroup takes one expert and 64 (16-bit types: 128) columns; where that leaves
+// How a call is shared out.  A panel of weights is multiplied by as many tiles of 16 tokens as most experts will
+// have (an even share and half as much again); an expert with more reads its weights again.  Fewer tiles leave registers for
+// more workgroups per CU.  A workgroup takes one expert and 64 (16-bit types: 128) columns; where that leaves
 // fewer than 256 workgroups, half as many columns.  The second product is also cut along its
 // rows, into at most one stage of 32 rows per wave, until there are 512 workgroups.  Its parts are joined by the last
 // workgroup of each column block where that has one value per thread or less, else (a few workgroups would
@@ -442,7 +454,7 @@ __global__ __launch_bounds__(256) void expert_join_kernel(ExpertArgs a, const fl
 // first product where the router is small (up to 256 KB, read from L2 in little more than the time of the
 // launch that this saves).
 struct ExpertPlan {
-  int experts, cols_up, cols_down, splits, rows_per_split;
+  int experts, cols_up, cols_down, splits, rows_per_split, tiles;
   bool join, route_inside;
 };
 static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
@@ -458,6 +470,8 @@ static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
   q.splits = want < most ? want : most;
   q.rows_per_split = (int)cdiv(cdiv(p->d_hidden, q.splits), 32) * 32;
   q.splits = (int)cdiv(p->d_hidden, q.rows_per_split);
+  const int share = cdiv(3ll * slots, 2ll * p->n_experts), all = tokens < share ? tokens : share;
+  q.tiles = all <= 16 ? 1 : all <= 32 ? 2 : 4;
   q.join = tokens * 16 * q.cols_down <= 64 * kExpertWaves;
   q.route_inside = tokens == 1 && (long long)p->d * p->n_experts <= 65536;
   return q;
@@ -527,12 +541,12 @@ extern "C" int janus_expert_layer(const janus_experts* p, const void* x, int64_t
       else f(std::integral_constant<int, kWide / 2>{});
     };
     auto by_tiles = [&](auto f) {
-      if (tokens <= 16) f(std::integral_constant<int, 1>{});
-      else if (tokens <= 32) f(std::integral_constant<int, 2>{});
+      if (plan.tiles == 1) f(std::integral_constant<int, 1>{});
+      else if (plan.tiles == 2) f(std::integral_constant<int, 2>{});
       else f(std::integral_constant<int, 4>{});
     };
     auto by_router = [&](auto f) {
-      if (a.n % 4 == 0 && rows_aligned(a.router, 0, 4)) f(std::integral_constant<int, 4>{});
+      if (a.n >= 4) f(std::integral_constant<int, 4>{});
       else f(std::integral_constant<int, 1>{});
     };
     auto launch_up = [&](auto cols, auto mt, auto v, auto routes) {

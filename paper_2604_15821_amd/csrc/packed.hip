@@ -28,7 +28,9 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, int c, int d, f
     load_run<T, 8>(row + c, v);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? (float)row[c + j] : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = (float)row[min(c + j, d - 1)];   // all at once, then cut off
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? v[j] : 0.f;
   }
 }
 template <typename T>
@@ -163,8 +165,9 @@ __device__ __forceinline__ unsigned pack_high(float a, float b) {   // the upper
 __device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
 
 // Where the rows of both operands start on 16 bytes (WIDE), a chunk's rows are a buffer: reads behind its last
-// value give zero, so its ragged end needs no code.  Other rows are read by runs at any address, up to the last
-// whole one, and value by value from there; rows behind the chunk are skipped.
+// value give zero, so its ragged end needs no code.  Other rows are read by runs at any address too: past a row's
+// end a run goes on into the next one (those columns are not stored), and only at the very end of the array are
+// values read one by one.  Rows behind the chunk are read as its last one and cleared before they are used.
 typedef __amdgpu_buffer_rsrc_t buffer;
 __device__ __forceinline__ buffer rows_buffer(const void* p, unsigned bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
@@ -185,13 +188,17 @@ struct Octet {
       for (int i = 0; i < V; ++i) v[j + i] = u[i];
     }
   }
-  __device__ __forceinline__ void load(const T* __restrict__ row, int c, int n) {   // n = 0: no row
-    if (c + 8 <= n) {
-      __builtin_memcpy(v, row + c, sizeof v);
+  __device__ __forceinline__ void load(const T* __restrict__ b, long long at, long long end) {
+    if (at + 8 <= end) {
+      __builtin_memcpy(v, b + at, sizeof v);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c + j < n ? row[c + j] : (T)0.f;
+      for (int j = 0; j < 8; ++j) v[j] = b[min(at + j, end - 1)];
     }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (T)0.f;
   }
   __device__ __forceinline__ void planes(uint4 (&o)[Terms<T>::kPlanes]) const {
     if constexpr (Terms<T>::kPlanes == 1) {
@@ -222,16 +229,16 @@ struct Sixteen {
     q = (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0);
     code = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(codes, at_code, 0, 0);
   }
-  __device__ __forceinline__ void load(const int8_t* __restrict__ row, const uint8_t* __restrict__ codes, int c, int n) {
-    if (c + 16 <= n) {
-      __builtin_memcpy(&q, row + c, 16);
+  __device__ __forceinline__ void load(const int8_t* __restrict__ x, long long at, long long end, int c) {
+    if (at + 16 <= end) {
+      __builtin_memcpy(&q, x + at, 16);
     } else {
-      q = u32x4{};
+      int8_t v[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (c + j < n) q[j >> 2] |= (unsigned)(uint8_t)row[c + j] << (8 * (j & 3));
+      for (int j = 0; j < 16; ++j) v[j] = x[min(at + j, end - 1)];
+      __builtin_memcpy(&q, v, 16);
     }
-    code = c < n ? codes[c / kPackBlock] : 0;
+    code = c;
   }
   // the half `first` of them, then the other
   __device__ __forceinline__ void values(int first, uint4 (&o)[2]) const {
@@ -271,8 +278,8 @@ __device__ __forceinline__ unsigned last_byte(int rows, long long ld, int width,
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __restrict__ q, long long ldq,
                                                               const uint8_t* __restrict__ code, long long ldc,
-                                                              const T* __restrict__ b, long long ldb, int P, int Q,
-                                                              const PackedChunk* __restrict__ chunks,
+                                                              const T* __restrict__ b, long long ldb, long long n_rows,
+                                                              int P, int Q, const PackedChunk* __restrict__ chunks,
                                                               const int* __restrict__ n_chunks, int tiles_p,
                                                               int tiles_q, float* __restrict__ partial,
                                                               float* __restrict__ G) {
@@ -315,17 +322,26 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
       atC += kWgRows * (unsigned)ldc;
       atB += stepB;
     } else {
-      const long long ra = ahead + ma;
-      r.a.load(q + ra * ldq, code + ra * ldc, p0 + 16 * ua, ra < ch.r1 ? P : 0);
+      const long long ra = min(ahead + ma, ch.r1 - 1);
+      const int cA = p0 + 16 * ua;
+      r.a.load(q, ra * ldq + cA, (n_rows - 1) * ldq + P, code[ra * ldc + min(cA, P - 1) / kPackBlock]);
 #pragma unroll
-      for (int i = 0; i < kPass; ++i) {
-        const long long rb = ahead + mb + i * kRowsPass;
-        r.b[i].load(b + rb * ldb, c0 + 8 * ob, rb < ch.r1 ? Q : 0);
-      }
+      for (int i = 0; i < kPass; ++i)
+        r.b[i].load(b, min(ahead + mb + i * kRowsPass, ch.r1 - 1) * ldb + c0 + 8 * ob, (n_rows - 1) * ldb + Q);
       ahead += kWgRows;
     }
   };
-  auto stage = [&](const Regs& r, char* to) {
+  int staged = ch.r0;
+  auto stage = [&](Regs& r, char* to) {
+    if constexpr (!WIDE) {
+      if (staged + kWgRows > ch.r1) {
+        if (staged + ma >= ch.r1) r.a.code = 0;   // a scale of zero
+#pragma unroll
+        for (int i = 0; i < kPass; ++i)
+          if (staged + mb + i * kRowsPass >= ch.r1) r.b[i].clear();
+      }
+      staged += kWgRows;
+    }
     uint4 o[2];   // odd rows write their second half first: two rows then fill all banks
     r.a.values(half, o);
     *reinterpret_cast<uint4*>(to + wa + 16 * half) = o[0];
@@ -378,10 +394,6 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
 
   Regs r0, r1;
   const int steps = (rows + kWgRows - 1) / kWgRows;
-  load(r0);
-  stage(r0, lds);
-  load(r0);
-  __syncthreads();
   // multiplies the stage in `from` while `next` holds the one after it and `after` is loaded with the next but one
   auto step = [&](const char* from, char* to, Regs& next, Regs& after) {
     load(after);
@@ -389,6 +401,12 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
     stage(next, to);
     __syncthreads();
   };
+  if (steps > 0) {
+    load(r0);
+    stage(r0, lds);
+    load(r0);
+    __syncthreads();
+  }
   for (int s = 0; s < steps; s += 2) {
     step(lds, lds + kStage, r0, r1);
     if (s + 1 < steps) step(lds + kStage, lds, r1, r0);
@@ -594,7 +612,7 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
     using T = decltype(zero);
     auto go = [&](auto is_wide) {
       hipLaunchKernelGGL((packed_wgrad_kernel<T, decltype(is_wide)::value>), dim3((unsigned)blocks), dim3(256), 0, st, q,
-                         ldq, code, ldc, static_cast<const T*>(B), ldb, P, Q, chunks, n_chunks, w.tiles_p, w.tiles_q,
+                         ldq, code, ldc, static_cast<const T*>(B), ldb, rows, P, Q, chunks, n_chunks, w.tiles_p, w.tiles_q,
                          partial, G);
     };
     if (wide) go(std::true_type{});
