@@ -288,10 +288,16 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   constexpr int kRowA = kWgP * 2, kRowB = COLS * 2, kBytesA = kWgRows * kRowA, kBytesB = kWgRows * kRowB;
   constexpr int kStage = kBytesA + NP * kBytesB;
   __shared__ __align__(16) char lds[2 * kStage];
-  // block -> die block % 8 -> chunk, tile: the tiles of a chunk are consecutive blocks of one die
-  const int tiles = tiles_p * tiles_q, slot = blockIdx.x >> 3;
-  const int at = slot / tiles * 8 + (blockIdx.x & 7), tile = slot % tiles;
-  if (at >= *n_chunks) return;
+  // block -> die block % 8 -> chunk, tile: the tiles of a chunk are consecutive blocks of one die; fewer chunks than
+  // dies are cut into eight equal runs of tiles
+  const int tiles = tiles_p * tiles_q, slot = blockIdx.x >> 3, die = blockIdx.x & 7, all = *n_chunks;
+  int at = slot / tiles * 8 + die, tile = slot % tiles;
+  if (all < 8) {
+    const int per = (all * tiles + 7) / 8, i = die * per + slot;
+    at = slot < per ? i / tiles : all;
+    tile = i % tiles;
+  }
+  if (at >= all) return;
   const PackedChunk ch = chunks[at];
   const int p0 = tile / tiles_q * kWgP, c0 = tile % tiles_q * COLS;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -493,16 +499,20 @@ struct WgradPlan {
   int tiles_p, tiles_q, kc, most;
   int64_t chunks, first, count, partial, total;   // offsets in bytes
 };
-// The chunk length: half of what each of 512 resident workgroups would get of all stages, so that the last ones end
-// together; not below 512 rows, where partials cost more than they save (20 000 rows, one group, 256 x 256, fp32: 37 us at 256,
-// 30 at 512), nor above 16 384, so that a chunk's
-// bytes stay within the 32-bit offsets of a buffer for rows of up to 256 KB.
-constexpr int kMostChunkRows = 16384;
+// The chunk length.  Where at least half of the 512 resident workgroups are left after one more chunk per group (whose
+// last chunks are ragged), chunks that fill them in one round; else half of what each would get of all rows, so
+// that the last ones end together.  (One group of 65 536 rows, 512 x 2048, bf16: 227 us by the second rule, 185 by the first.)
+// Not below 512 rows, where partials cost more than they save (20 000 rows, one group, 256 x 256, fp32: 30 us at 512,
+// 38 at 256), nor above 16 384, so that a chunk's bytes stay within the 32-bit offsets of a buffer for rows of up to
+// 256 KB.
+constexpr int kMostChunkRows = 16384, kWgSlots = 512;
 static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
   WgradPlan w;
   w.tiles_p = (int)cdiv(P, kWgP);
   w.tiles_q = (int)cdiv(Q, type == JANUS_BF16 ? Terms<__bf16>::kCols : Terms<float>::kCols);
-  const double share = (double)rows * w.tiles_p * w.tiles_q / 1024;
+  const double work = (double)rows * w.tiles_p * w.tiles_q;   // rows of all tiles
+  const double room = kWgSlots - (double)(groups - 1) * w.tiles_p * w.tiles_q;
+  const double share = room >= kWgSlots / 2 ? work / room : work / (2 * kWgSlots);
   const double kc = share < 512 ? 512 : share > kMostChunkRows ? kMostChunkRows : share;
   w.kc = (int)((kc + kWgRows - 1) / kWgRows) * kWgRows;
   w.most = (int)(groups + rows / w.kc);
