@@ -172,3 +172,32 @@ def test_rows_apart_and_no_tokens():
     assert (out[:, :4] == 5).all() and (out[:, 68:] == 5).all()
     y, eid, gate = janus.expert_layer(q["x"][:0], q["router"], q["w_up"], q["w_down"], 2)
     assert y.shape == (0, 64) and eid.shape == (0, 2) and gate.shape == (0, 2)
+
+
+def test_small_and_large_fp16_weights():
+    """Subnormal fp16 weights and hidden values beyond fp16's range take part like others."""
+    import torch
+    banner("expert_layer fp16 range")
+    s = _case(5, 6, 64, 96, 3, "f16")
+    s["w_up"] = (s["w_up"].float() * 2.0 ** -20).to(torch.float16)
+    s["x"] = (s["x"].float() * 2.0 ** 10).to(torch.float16)
+    s["router"] = s["router"] * 2.0 ** -10
+    _check(s, 2, False, "f16", _run(s, 2))
+    s = _case(6, 6, 64, 96, 3, "f16")
+    s["x"] = (s["x"].float() * 2.0 ** 12).to(torch.float16)
+    s["w_up"] = (s["w_up"].float() * 2.0 ** 7).to(torch.float16)
+    s["w_down"] = (s["w_down"].float() * 2.0 ** -20).to(torch.float16)
+    s["router"] = s["router"] * 2.0 ** -12
+    got = _run(s, 2)
+    assert torch.isfinite(got[0]).all()
+    _check(s, 2, False, "f16", got)
+
+
+def test_more_tokens_on_an_expert_than_planned():
+    """A few experts get nearly all tokens, though an even share is a fraction of a tile."""
+    import torch
+    banner("expert_layer skewed")
+    s = _case(7, 61, 96, 160, 40, "f32")
+    s["beta"] = torch.zeros(40)
+    s["beta"][[4, 30]] = 50.0
+    _check(s, 3, False, "f32", _run(s, 3))

@@ -176,6 +176,29 @@ def test_wgrad(sizes, P, Q, t):
     _wgrad_check(p, b, off, G, t)
 
 
+@pytest.mark.parametrize("groups", [64, 65, 300, 1024])
+def test_wgrad_many_groups(groups):
+    """Some groups are empty, and one is long enough for several chunks."""
+    import numpy as np
+    from paper_2604_15821_amd import janus
+    banner("packed_wgrad groups", groups)
+    sizes = np.random.default_rng(groups).integers(0, 20, groups)
+    sizes[groups // 3] = 2500
+    x, b, off = _wgrad_case(groups, sizes.tolist(), 24, 16, "bf16")
+    p = janus.pack_rows(x.cuda())
+    _wgrad_check(p, b, off, janus.packed_wgrad(p, b.cuda(), off.cuda()), "bf16")
+
+
+@pytest.mark.parametrize("rows,P,Q", [(9000, 300, 520), (4000, 1024, 1030), (1200, 2048, 64)])
+def test_wgrad_one_group(rows, P, Q):
+    """Fewer chunks than dies, with many tiles each."""
+    from paper_2604_15821_amd import janus
+    banner("packed_wgrad one group", rows, P, Q)
+    x, b, off = _wgrad_case(rows, [rows], P, Q, "f16")
+    p = janus.pack_rows(x.cuda())
+    _wgrad_check(p, b, off, janus.packed_wgrad(p, b.cuda(), off.cuda()), "f16")
+
+
 @pytest.mark.parametrize("t", TYPES)
 def test_wgrad_many_rows(t):
     """Long groups (several chunks each) and the same result on every run."""
