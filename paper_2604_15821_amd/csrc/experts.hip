@@ -278,15 +278,17 @@ __device__ __forceinline__ int find_slots(const ExpertArgs& a, const int* __rest
   return s.count;
 }
 
-// One expert's slots base .. base + 16 MT - 1 times COLS * 16 columns of its weight, over the rows [k0, k1) of it; the
-// waves take stages of 32 rows in turn and are added in order.  done(t, c, v): value of the t-th slot in column c.
+// One expert's slots base .. base + 16 MT - 1 times columns of its weight, over the rows [k0, k1) of it.  `deep` waves
+// (a power of two) share COLS * 16 columns: they take stages of 32 rows in turn and are added in order; the
+// workgroup owns kExpertWaves / deep such blocks of columns.  done(t, c, v): value of the t-th slot in column c.
 // `A` is the operand of a token's values S, row ld apart, slot q reading row q / per.
 template <typename T, typename S, typename A, int COLS, int MT, typename F>
 __device__ __forceinline__ void expert_product(const ExpertSlots& s, int base, const S* __restrict__ x, long long ldx, int per,
-                                               const T* __restrict__ w, int n, int k0, int k1, int K,
+                                               const T* __restrict__ w, int n, int k0, int k1, int K, int deep,
                                                float* __restrict__ lds, F done) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = 8 * (lane >> 4);
-  const int c0 = blockIdx.x * (16 * COLS);
+  const int across = kExpertWaves / deep, level = wave & (deep - 1);
+  const int first = blockIdx.x * across * (16 * COLS), c0 = first + wave / deep * (16 * COLS);
   // columns past the end (n is a multiple of 16, so of COLS) read the last ones and are not stored
   const T* wl = w + min(c0 + COLS * (lane & 15), n - COLS);
   const int count = min(s.count - base, 16 * MT), tiles = (count + 15) >> 4;
@@ -299,11 +301,11 @@ __device__ __forceinline__ void expert_product(const ExpertSlots& s, int base, c
 #pragma unroll
     for (int c = 0; c < COLS; ++c) acc[m][c] = f32x4{};
   Panel<T, COLS> now, next;
-  int k = k0 + 32 * wave;
+  int k = k0 + 32 * level;
   if (k < k1) now.load(wl, n, k + sub, K);
-  for (; k < k1; k += 32 * kExpertWaves) {
-    const bool more = k + 32 * kExpertWaves < k1;
-    if (more) next.load(wl, n, k + 32 * kExpertWaves + sub, K);
+  for (; k < k1; k += 32 * deep) {
+    const bool more = k + 32 * deep < k1;
+    if (more) next.load(wl, n, k + 32 * deep + sub, K);
     const bool behind = k + sub >= k1;
     if (behind) now.clear();
 #pragma unroll
@@ -331,14 +333,29 @@ __device__ __forceinline__ void expert_product(const ExpertSlots& s, int base, c
     }
     __syncthreads();
     const int rows = min(16, count - 16 * m);
-    for (int e = threadIdx.x; e < rows * 16 * COLS; e += 64 * kExpertWaves) {
+    const int part = rows * 16 * COLS;
+    for (int e = threadIdx.x; e < across * part; e += 64 * kExpertWaves) {
       float v = 0.f;
+      int block = 0, i = e;
+      if (deep == kExpertWaves) {
 #pragma unroll
-      for (int q = 0; q < kExpertWaves; ++q) v += lds[q * (256 * COLS) + e];
-      const int c = c0 + e % (16 * COLS);
-      if (c < n) done(base + 16 * m + e / (16 * COLS), c, v);
+        for (int q = 0; q < kExpertWaves; ++q) v += lds[q * (256 * COLS) + i];
+      } else {
+        block = e / part;
+        i = e - block * part;
+        for (int q = 0; q < deep; ++q) v += lds[(block * deep + q) * (256 * COLS) + i];
+      }
+      const int c = first + block * (16 * COLS) + i % (16 * COLS);
+      if (c < n) done(base + 16 * m + i / (16 * COLS), c, v);
     }
   }
+}
+
+// Waves that share a block of columns of a product over `rows` rows: one per stage, at most all.
+__host__ __device__ inline int deep_waves(int rows) {
+  int deep = 1;
+  while (deep < kExpertWaves && 32 * deep < rows) deep <<= 1;
+  return deep;
 }
 
 // hidden[slot, j] = SiLU(sum_i x[i] W1[e, i, j])
@@ -365,7 +382,7 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs
     if (find_slots(a, eid, s) == 0) return;
   }
   for (int base = 0; base < s.count; base += 16 * MT)
-    expert_product<T, T, Eight<T>, COLS, MT>(s, base, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d, a.d, lds,
+    expert_product<T, T, Eight<T>, COLS, MT>(s, base, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d, a.d, deep_waves(a.d), lds,
                                            [&](int t, int c, float v) {
                                              hidden[(long long)s.slot[t] * a.h + c] = silu(v);
                                            });
@@ -410,10 +427,10 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_down_kernel(ExpertAr
   __shared__ float lds[kExpertWaves * 256 * COLS];
   __shared__ int last;
   const int splits = gridDim.z, k0 = blockIdx.z * rows_per_split;
-  const int count = find_slots(a, eid, s);
+  const int count = find_slots(a, eid, s), deep = deep_waves(rows_per_split);
   for (int base = 0; base < count; base += 16 * MT)
     expert_product<T, float, A, COLS, MT>(s, base, hidden, a.h, 1, w2 + (long long)s.expert * a.h * a.d, a.d, k0,
-                                          min(k0 + rows_per_split, a.h), a.h, lds, [&](int t, int c, float v) {
+                                          min(k0 + rows_per_split, a.h), a.h, deep, lds, [&](int t, int c, float v) {
                                             float* o = part + ((long long)s.slot[t] * splits + blockIdx.z) * a.d + c;
                                             if constexpr (kJoin)
                                               __hip_atomic_store(o, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -426,9 +443,9 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_down_kernel(ExpertAr
     if (threadIdx.x == 0) last = atomicAdd(arrived + blockIdx.x, 1) == (int)(gridDim.y * gridDim.z) - 1;
     __syncthreads();
     if (!last) return;
-    const int c0 = blockIdx.x * (16 * COLS);
-    for (int e = threadIdx.x; e < a.tokens * 16 * COLS; e += 64 * kExpertWaves) {
-      const int t = e / (16 * COLS), c = c0 + e % (16 * COLS);
+    const int width = kExpertWaves / deep * (16 * COLS);
+    for (int e = threadIdx.x; e < a.tokens * width; e += 64 * kExpertWaves) {
+      const int t = e / width, c = blockIdx.x * width + e % width;
       if (c < a.d)
         y[t * ldy + c] = (T)expert_sum(a, gate, part, splits, t, c, [](float* p) {
           return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -446,33 +463,38 @@ __global__ __launch_bounds__(256) void expert_join_kernel(ExpertArgs a, const fl
 
 // How a call is shared out.  A panel of weights is multiplied by as many tiles of 16 tokens as most experts will
 // have (an even share and half as much again); an expert with more reads its weights again.  Fewer tiles leave registers for
-// more workgroups per CU.  A workgroup takes one expert and 64 (16-bit types: 128) columns; where that leaves
-// fewer than 256 workgroups, half as many columns.  The second product is also cut along its
+// more workgroups per CU.  A wave takes 64 (16-bit types: 128) columns of an expert, where that leaves fewer than 256
+// workgroups half as many; all eight waves of a workgroup the same ones if there are stages for them, else more
+// columns (d = 64, h = 3536, 128 experts, 44 tokens, bf16: 44 us with idle waves, 37 without).  The second product is also cut along its
 // rows, into at most one stage of 32 rows per wave, until there are 512 workgroups.  Its parts are joined by the last
 // workgroup of each column block where that has one value per thread or less, else (a few workgroups would
 // join for long while the others idle) by a kernel of their own.  One token is routed by every workgroup of the
 // first product where the router is small (up to 256 KB, read from L2 in little more than the time of the
 // launch that this saves).
 struct ExpertPlan {
-  int experts, cols_up, cols_down, splits, rows_per_split, tiles;
+  int experts, cols_up, cols_down, blocks_up, blocks_down, splits, rows_per_split, tiles;
   bool join, route_inside;
 };
 static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
   ExpertPlan q;
   const int slots = tokens * p->top_k, wide = p->type == JANUS_F32 ? 4 : 8;
   q.experts = slots < p->n_experts ? slots : p->n_experts;
-  auto cols = [&](int n) { return (long long)q.experts * cdiv(n, 16 * wide) < 256 ? wide / 2 : wide; };
-  q.cols_up = cols(p->d_hidden);
-  q.cols_down = cols(p->d);
-  const long long blocks = (long long)q.experts * cdiv(p->d, 16 * q.cols_down);
+  auto blocks = [&](int n, int cols, int rows) { return (int)cdiv(n, 16 * cols * (kExpertWaves / deep_waves(rows))); };
+  auto columns = [&](int n, int rows) {
+    return (long long)q.experts * blocks(n, wide, rows) < 256 ? wide / 2 : wide;
+  };
+  q.cols_up = columns(p->d_hidden, p->d);
+  q.cols_down = columns(p->d, p->d_hidden);
+  q.blocks_up = blocks(p->d_hidden, q.cols_up, p->d);
   const int stage = 32 * kExpertWaves, most = (int)cdiv(p->d_hidden, stage);
-  const int want = (int)cdiv(512, blocks);
+  const int want = (int)cdiv(512, (long long)q.experts * blocks(p->d, q.cols_down, p->d_hidden));
   q.splits = want < most ? want : most;
   q.rows_per_split = (int)cdiv(cdiv(p->d_hidden, q.splits), 32) * 32;
   q.splits = (int)cdiv(p->d_hidden, q.rows_per_split);
+  q.blocks_down = blocks(p->d, q.cols_down, q.rows_per_split);
   const int share = cdiv(3ll * slots, 2ll * p->n_experts), all = tokens < share ? tokens : share;
   q.tiles = all <= 16 ? 1 : all <= 32 ? 2 : 4;
-  q.join = tokens * 16 * q.cols_down <= 64 * kExpertWaves;
+  q.join = (long long)tokens * cdiv(p->d, q.blocks_down) <= 64 * kExpertWaves;
   q.route_inside = tokens == 1 && (long long)p->d * p->n_experts <= 65536;
   return q;
 }
@@ -485,7 +507,7 @@ static ExpertWork expert_work(const janus_experts* p, int tokens, const ExpertPl
   w.hidden = 0;
   w.part = w.hidden + 4 * slots * p->d_hidden;
   w.arrived = w.part + 4 * slots * q.splits * p->d;
-  w.total = w.arrived + 4 * ((cdiv(p->d, 16 * q.cols_down) + 3) / 4 * 4);
+  w.total = w.arrived + 4 * ((q.blocks_down + 3) / 4 * 4);
   return w;
 }
 
@@ -532,7 +554,7 @@ extern "C" int janus_expert_layer(const janus_experts* p, const void* x, int64_t
   int* arrived = reinterpret_cast<int*>(base + at.arrived);
   with_type(p->type, [&](auto zero) {
     using T = decltype(zero);
-    const int counts = (int)cdiv(a.d, 16 * plan.cols_down);
+    const int counts = plan.blocks_down;
     const T* xt = static_cast<const T*>(x);
     const T* up = static_cast<const T*>(p->w_up);
     auto by_columns = [&](int cols, auto f) {
@@ -551,12 +573,12 @@ extern "C" int janus_expert_layer(const janus_experts* p, const void* x, int64_t
     };
     auto launch_up = [&](auto cols, auto mt, auto v, auto routes) {
       hipLaunchKernelGGL((expert_up_kernel<T, cols.value, mt.value, v.value, routes.value>),
-                         dim3(cdiv(a.h, 16 * cols.value), plan.experts), dim3(64 * kExpertWaves), 0, st, a, xt, ldx, up,
+                         dim3(plan.blocks_up, plan.experts), dim3(64 * kExpertWaves), 0, st, a, xt, ldx, up,
                          eid, gate, arrived, counts, hidden);
     };
     auto launch_down = [&](auto cols, auto mt, auto join) {
       hipLaunchKernelGGL((expert_down_kernel<T, cols.value, mt.value, join.value>),
-                         dim3(cdiv(a.d, 16 * cols.value), plan.experts, plan.splits), dim3(64 * kExpertWaves), 0, st, a,
+                         dim3(plan.blocks_down, plan.experts, plan.splits), dim3(64 * kExpertWaves), 0, st, a,
                          hidden, static_cast<const T*>(p->w_down), eid, gate, part, arrived, plan.rows_per_split,
                          static_cast<T*>(y), ldy);
     };

@@ -164,10 +164,11 @@ __device__ __forceinline__ unsigned pack_high(float a, float b) {   // the upper
 }
 __device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
 
-// Where the rows of both operands start on 16 bytes (WIDE), a chunk's rows are a buffer: reads behind its last
-// value give zero, so its ragged end needs no code.  Other rows are read by runs at any address too: past a row's
-// end a run goes on into the next one (those columns are not stored), and only at the very end of the array are
-// values read one by one.  Rows behind the chunk are read as its last one and cleared before they are used.
+// Where the rows of both operands start on four bytes (WORDS: always for fp32), a chunk's rows are a buffer: words
+// behind the one that holds its last value are zero, so its ragged end needs no code.  Past a row's end a run goes on
+// into the next one; those columns are not stored.  Other rows are read by runs at any address in the same way, but
+// at the very end of the array value by value, and rows behind the chunk are read as its last one and cleared
+// before they are used.
 typedef __amdgpu_buffer_rsrc_t buffer;
 __device__ __forceinline__ buffer rows_buffer(const void* p, unsigned bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
@@ -269,13 +270,13 @@ __device__ __forceinline__ bf16x8 read_columns(const char* lo, const char* hi) {
 // Where a row's 32-byte unit lies.
 __device__ __forceinline__ int place(int unit, int m) { return unit ^ (2 * (m & 3)); }
 
-// Bytes of `rows` rows up to the last one's last value, rounded up to the `unit` by which they are read.
+// Bytes of `rows` rows up to the last one's last value, in units of what one read takes.
 __device__ __forceinline__ unsigned last_byte(int rows, long long ld, int width, int size, unsigned unit) {
   const unsigned n = rows ? (unsigned)(((rows - 1) * ld + width) * size) : 0u;
   return (n + unit - 1) & ~(unit - 1);
 }
 
-template <typename T, bool WIDE>
+template <typename T, bool WORDS>
 __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __restrict__ q, long long ldq,
                                                               const uint8_t* __restrict__ code, long long ldc,
                                                               const T* __restrict__ b, long long ldb, long long n_rows,
@@ -304,9 +305,9 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
 
   // staging: thread t holds 16 values of X's row t / 8 and, per pass, 8 values of a row of B
   const int rows = ch.r1 - ch.r0;
-  const buffer bufA = rows_buffer(q + ch.r0 * ldq, last_byte(rows, ldq, P, 1, 16));
+  const buffer bufA = rows_buffer(q + ch.r0 * ldq, last_byte(rows, ldq, P, 1, 4));
   const buffer bufC = rows_buffer(code + ch.r0 * ldc, last_byte(rows, ldc, (P + kPackBlock - 1) / kPackBlock, 1, 1));
-  const buffer bufB = rows_buffer(b + ch.r0 * ldb, last_byte(rows, ldb, Q, sizeof(T), 16));
+  const buffer bufB = rows_buffer(b + ch.r0 * ldb, last_byte(rows, ldb, Q, sizeof(T), 4));
   const int ma = t >> 3, ua = t & 7, half = ma & 1;
   const int wa = ma * kRowA + (place(ua, ma) << 5);
   constexpr int kPerRow = COLS / 8, kRowsPass = 256 / kPerRow;
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   };
   int ahead = ch.r0;   // the next stage's first row
   auto load = [&](Regs& r) {
-    if constexpr (WIDE) {
+    if constexpr (WORDS) {
       r.a.load(bufA, atA, bufC, atC);
 #pragma unroll
       for (int i = 0; i < kPass; ++i) r.b[i].load(bufB, atB + i * passB);
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   };
   int staged = ch.r0;
   auto stage = [&](Regs& r, char* to) {
-    if constexpr (!WIDE) {
+    if constexpr (!WORDS) {
       if (staged + kWgRows > ch.r1) {
         if (staged + ma >= ch.r1) r.a.code = 0;   // a scale of zero
 #pragma unroll
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const int row = p + 8 * (k >> 2) + (k & 3);
-          if (row < P) __builtin_nontemporal_store(acc[i][f][k], out + (long long)row * Q + c);
+          if (row < P) out[(long long)row * Q + c] = acc[i][f][k];
         }
       }
     }
@@ -617,15 +618,15 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(packed_chunks_kernel, dim3(1), dim3(1024), 0, st, row_off, n_groups, rows, w.kc, chunks, w.most,
                      n_chunks, first, count);
-  const bool wide = rows_aligned(q, ldq, 1) && rows_aligned(B, ldb, type_bytes(type));
+  const bool words = rows_aligned(q, ldq, 1, 4) && rows_aligned(B, ldb, type_bytes(type), 4);
   with_type(type, [&](auto zero) {
     using T = decltype(zero);
-    auto go = [&](auto is_wide) {
-      hipLaunchKernelGGL((packed_wgrad_kernel<T, decltype(is_wide)::value>), dim3((unsigned)blocks), dim3(256), 0, st, q,
+    auto go = [&](auto in_words) {
+      hipLaunchKernelGGL((packed_wgrad_kernel<T, decltype(in_words)::value>), dim3((unsigned)blocks), dim3(256), 0, st, q,
                          ldq, code, ldc, static_cast<const T*>(B), ldb, rows, P, Q, chunks, n_chunks, w.tiles_p, w.tiles_q,
                          partial, G);
     };
-    if (wide) go(std::true_type{});
+    if (words) go(std::true_type{});
     else go(std::false_type{});
   });
   const int64_t PQ = (int64_t)P * Q;
