@@ -3,6 +3,7 @@
 //   l = x Wr + beta;  the top_k largest of a token, lower index first on ties
 //   g = softmax(l) of the chosen (normalize: divided by their sum)
 //   y = sum_c g_c W2_c^T SiLU(W1_c^T x)
+#include <algorithm>
 #include <type_traits>
 
 #include "rows.h"
@@ -12,6 +13,7 @@ namespace janus {
 constexpr int kExpertTokens = 64;   // tokens of a call, at most
 constexpr int kMaxExperts = 256;
 constexpr int kMaxTopK = 8;
+constexpr int kMostShares = 16;     // of a large router's rows
 
 struct ExpertArgs {
   int tokens, d, h, n, k, normalize;
@@ -32,15 +34,16 @@ struct RouteArea {
   float sum[4], top[kMaxTopK], gate[kMaxTopK];
   int eid[kMaxTopK], nan;
 };
+// logit parts of rows [begin, end): red[wave]
 template <typename T, int V, int W>
-__device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __restrict__ x, RouteArea<W>& s) {
+__device__ __forceinline__ void route_sums(const ExpertArgs& a, const T* __restrict__ x, int begin, int end,
+                                           RouteArea<W>& s) {
   typedef float vec __attribute__((ext_vector_type(V), aligned(4)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int units = (a.n + V - 1) / V;
   int wide = 1;
   while (wide < units && wide < 64) wide <<= 1;
   const int per = 64 / wide, rows = per * W, row0 = wave * per + lane / wide;
-  if (threadIdx.x == 0) s.nan = 0;
   for (int u0 = 0; u0 < units; u0 += 64) {
     const int u = u0 + (lane & (wide - 1)), c0 = max(min(V * u, a.n - V), 0);
     vec sum = {};
@@ -50,16 +53,16 @@ __device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __rest
       float v[flight.value];
 #pragma unroll
       for (int j = 0; j < flight.value; ++j) {
-        const int q = min(i + j * rows, a.d - 1);
+        const int q = min(i + j * rows, end - 1);
         r[j] = *reinterpret_cast<const vec*>(w + (long long)q * a.n);
         v[j] = (float)x[q];
       }
 #pragma unroll
       for (int j = 0; j < flight.value; ++j)
-        if (i + j * rows < a.d) sum += r[j] * v[j];
+        if (i + j * rows < end) sum += r[j] * v[j];
     };
-    for (int i = 0; i < a.d;) {
-      if (i + 8 * rows < a.d) {
+    for (int i = begin; i < end;) {
+      if (i + 8 * rows < end) {
         add(std::integral_constant<int, 16>{}, i + row0);
         i += 16 * rows;
       } else {
@@ -74,15 +77,28 @@ __device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __rest
     }
   }
   __syncthreads();
-  const int e = threadIdx.x;
-  float l = -INFINITY, key = -INFINITY;
-  if (e < a.n) {
-    l = 0.f;
+}
+template <int W>
+__device__ __forceinline__ float route_sum(const RouteArea<W>& s, int e) {
+  float l = 0.f;
 #pragma unroll
-    for (int p = 0; p < W; ++p) l += s.red[p][e];
+  for (int p = 0; p < W; ++p) l += s.red[p][e];
+  return l;
+}
+
+// The choice from the logit l of expert threadIdx.x, before beta.
+template <int W>
+__device__ __forceinline__ void route_choose(const ExpertArgs& a, float l, RouteArea<W>& s) {
+  const int e = threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (e == 0) s.nan = 0;
+  __syncthreads();
+  float key = -INFINITY;
+  if (e < a.n) {
     if (a.beta) l += a.beta[e];
     if (l == l) key = l;
     else s.nan = 1;
+  } else {
+    l = -INFINITY;
   }
   if (e < kMaxExperts) s.key[e] = key;
   __syncthreads();
@@ -114,6 +130,12 @@ __device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __rest
   __syncthreads();
 }
 
+template <typename T, int V, int W>
+__device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __restrict__ x, RouteArea<W>& s) {
+  route_sums<T, V, W>(a, x, 0, a.d, s);
+  route_choose(a, (int)threadIdx.x < a.n ? route_sum(s, threadIdx.x) : 0.f, s);
+}
+
 constexpr int kRouteWaves = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(64 * kRouteWaves) void expert_route_kernel(ExpertArgs a, const T* __restrict__ x,
@@ -129,6 +151,40 @@ __global__ __launch_bounds__(64 * kRouteWaves) void expert_route_kernel(ExpertAr
     eid[t * a.k + threadIdx.x] = s.eid[threadIdx.x];
     gate[t * a.k + threadIdx.x] = s.gate[threadIdx.x];
   }
+}
+
+// The same for a large router, of which one workgroup would read too much: blockIdx.x takes a share of the rows,
+// and a second kernel adds the shares in order and chooses.
+template <typename T, int V>
+__global__ __launch_bounds__(64 * kRouteWaves) void expert_logits_kernel(ExpertArgs a, const T* __restrict__ x,
+                                                                         long long ldx, int rows,
+                                                                         float* __restrict__ share) {
+  __shared__ RouteArea<kRouteWaves> s;
+  const int t = blockIdx.y, begin = blockIdx.x * rows;
+  route_sums<T, V, kRouteWaves>(a, x + t * ldx, begin, min(begin + rows, a.d), s);
+  const int e = threadIdx.x;
+  if (e < a.n) share[((long long)t * gridDim.x + blockIdx.x) * a.n + e] = route_sum(s, e);
+}
+__global__ __launch_bounds__(kMaxExperts) void expert_choose_kernel(ExpertArgs a, const float* __restrict__ share,
+                                                                    int shares, int* __restrict__ eid,
+                                                                    float* __restrict__ gate, int* __restrict__ arrived,
+                                                                    int n_arrived) {
+  __shared__ RouteArea<1> s;
+  const int t = blockIdx.x, e = threadIdx.x;
+  if (t == 0)
+    for (int i = e; i < n_arrived; i += kMaxExperts) arrived[i] = 0;
+  float l = 0.f;
+  if (e < a.n) {
+    const float* p = share + (long long)t * shares * a.n + e;
+    float v[kMostShares];
+#pragma unroll
+    for (int z = 0; z < kMostShares; ++z) v[z] = p[min(z, shares - 1) * a.n];
+#pragma unroll
+    for (int z = 0; z < kMostShares; ++z)
+      if (z < shares) l += v[z];
+  }
+  route_choose(a, l, s);
+  if (e < a.k) eid[t * a.k + e] = s.eid[e], gate[t * a.k + e] = s.gate[e];
 }
 
 // ------------------------------------------------------------------ the experts' products
@@ -470,9 +526,10 @@ __global__ __launch_bounds__(256) void expert_join_kernel(ExpertArgs a, const fl
 // workgroup of each column block where that has one value per thread or less, else (a few workgroups would
 // join for long while the others idle) by a kernel of their own.  One token is routed by every workgroup of the
 // first product where the router is small (up to 256 KB, read from L2 in little more than the time of the
-// launch that this saves).
+// launch that this saves); a larger router is shared out, 128 KB to a workgroup.
+constexpr int kRouterWhole = 65536;
 struct ExpertPlan {
-  int experts, cols_up, cols_down, blocks_up, blocks_down, splits, rows_per_split, tiles;
+  int experts, cols_up, cols_down, blocks_up, blocks_down, splits, rows_per_split, tiles, shares, rows_per_share;
   bool join, route_inside;
 };
 static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
@@ -495,7 +552,11 @@ static ExpertPlan expert_plan(const janus_experts* p, int tokens) {
   const int share = cdiv(3ll * slots, 2ll * p->n_experts), all = tokens < share ? tokens : share;
   q.tiles = all <= 16 ? 1 : all <= 32 ? 2 : 4;
   q.join = (long long)tokens * cdiv(p->d, q.blocks_down) <= 64 * kExpertWaves;
-  q.route_inside = tokens == 1 && (long long)p->d * p->n_experts <= 65536;
+  const long long router = (long long)p->d * p->n_experts;
+  q.route_inside = tokens == 1 && router <= kRouterWhole;
+  const int shares = router <= kRouterWhole ? 1 : (int)std::min<long long>(cdiv(router, kRouterWhole / 2), kMostShares);
+  q.rows_per_share = (int)cdiv(p->d, shares);
+  q.shares = (int)cdiv(p->d, q.rows_per_share);
   return q;
 }
 struct ExpertWork {
@@ -506,7 +567,9 @@ static ExpertWork expert_work(const janus_experts* p, int tokens, const ExpertPl
   ExpertWork w;
   w.hidden = 0;
   w.part = w.hidden + 4 * slots * p->d_hidden;
-  w.arrived = w.part + 4 * slots * q.splits * p->d;
+  // the router's shares are read before the parts are written
+  const int64_t parts = slots * q.splits * p->d, shares = q.shares > 1 ? (int64_t)tokens * q.shares * p->n_experts : 0;
+  w.arrived = w.part + (4 * std::max(parts, shares) + 15) / 16 * 16;
   w.total = w.arrived + 4 * ((q.blocks_down + 3) / 4 * 4);
   return w;
 }
@@ -587,9 +650,16 @@ extern "C" int janus_expert_layer(const janus_experts* p, const void* x, int64_t
       by_columns(plan.cols_up, [&](auto cols) { by_router([&](auto v) { launch_up(cols, one, v, std::true_type{}); }); });
     } else {
       by_router([&](auto v) {
-        hipLaunchKernelGGL((expert_route_kernel<T, v.value>), dim3(tokens), dim3(64 * kRouteWaves), 0, st, a, xt, ldx,
-                           eid, gate, arrived, counts);
+        if (plan.shares == 1)
+          hipLaunchKernelGGL((expert_route_kernel<T, v.value>), dim3(tokens), dim3(64 * kRouteWaves), 0, st, a, xt, ldx,
+                             eid, gate, arrived, counts);
+        else
+          hipLaunchKernelGGL((expert_logits_kernel<T, v.value>), dim3(plan.shares, tokens), dim3(64 * kRouteWaves), 0, st,
+                             a, xt, ldx, plan.rows_per_share, part);
       });
+      if (plan.shares > 1)
+        hipLaunchKernelGGL(expert_choose_kernel, dim3(tokens), dim3(kMaxExperts), 0, st, a, part, plan.shares, eid, gate,
+                           arrived, counts);
       by_columns(plan.cols_up,
                  [&](auto cols) { by_tiles([&](auto mt) { launch_up(cols, mt, one, std::false_type{}); }); });
     }

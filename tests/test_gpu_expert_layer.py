@@ -18,7 +18,7 @@ TYPES = ["f32", "bf16", "f16"]
 SHAPES = [(1, 16, 16, 1, 1, False), (1, 64, 128, 4, 1, False), (1, 512, 2048, 64, 2, False), (2, 128, 512, 8, 2, True),
           (3, 48, 80, 5, 5, False), (5, 144, 272, 33, 3, True), (13, 128, 512, 8, 2, False), (16, 96, 64, 3, 2, False),
           (17, 256, 192, 2, 1, False), (31, 64, 64, 256, 8, True), (33, 512, 1040, 7, 4, False), (64, 128, 512, 1, 1, False),
-          (64, 208, 336, 16, 8, True), (64, 1024, 512, 130, 6, False)]
+          (64, 208, 336, 16, 8, True), (64, 1024, 512, 130, 6, False), (1, 1600, 48, 200, 4, True), (3, 4112, 32, 253, 8, False)]
 
 
 def _dt(t):
