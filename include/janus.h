@@ -593,10 +593,11 @@ int janus_residual_norm_grad(const janus_norm* p /* host */, const void* dr, int
  *   type         janus_type of x, y, w_up and w_down
  *   router       [d, n_experts] fp32;  beta [n_experts] fp32 or NULL (-inf masks an expert out)
  *   w_up         [n_experts, d, d_hidden];  w_down [n_experts, d_hidden, d]; 16-byte aligned
- * x and y need rows that start on 16 bytes.  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
- * [tokens, top_k] fp32.  A token whose logits are all -inf gets gates of zero and y = 0; one with
- * a NaN logit gets gates and y of NaN.  Neither reaches other tokens.  The choice is exact up to the fp32
- * rounding of the logits.  y may not overlap x.
+ * x and y need rows that start on 16 bytes.  With 16-bit weights the hidden values enter the second product as two
+ * bf16 each (to 2^-16 of themselves, in fp32's range).  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
+ * [tokens, top_k] fp32; expert ids are always valid and distinct.  A token whose logits are all -inf gets
+ * gates of zero and y = 0; one with a logit of NaN or +inf gets gates and y of NaN.  Neither reaches other tokens.
+ * The choice is exact up to the fp32 rounding of the logits.  y may not overlap x.
  * Errors: JANUS_EINVAL (also misaligned arrays), JANUS_EUNSUPPORTED (sizes beyond these), JANUS_EHIP.
  */
 typedef struct janus_experts {
@@ -623,8 +624,7 @@ int janus_expert_layer(const janus_experts* p /* host */, const void* x, int64_t
  * each is off by at most max|x| / 127 of its block.  A block with an infinity or NaN gets c = 255
  * and q = 0 and reads as NaN.
  *   q [rows, d] int8, rows ldq apart;  code [rows, ceil(d / 32)] uint8, rows ldc apart.
- * Rows of q that start on multiples of 16 bytes are read and written fastest.  Columns of q between d and ldq are neither read
- * into a result nor written.
+ * Columns of q between d and ldq, and of code behind the last block, are neither read into a result nor written.
  */
 int janus_pack_rows(const void* x, int64_t ldx, int32_t type, int64_t rows, int32_t d, int8_t* q, int64_t ldq,
                     uint8_t* code, int64_t ldc, void* stream);
@@ -642,10 +642,12 @@ int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t
  * janus_grouped_wgrad that reads its left operand in 8 bits:
  *   G_g[p, c] = sum over the rows m of group g of X[m, p] B[m, c]
  * with X packed [rows, P], B [rows, Q] of `type`, G [n_groups, P, Q] fp32 and row_off [n_groups + 1]
- * int32 on the device, non-decreasing from 0 (row_off[n_groups] <= rows: rows behind the last group are not
- * read).  1..1024 groups, rows at most 2^31 - 4097; groups without rows get zeros.  Every product is exact in fp32, sums are held in
- * fp32 and split over row chunks that are added in a fixed order.  Offsets that break these rules
- * give wrong values but no access outside the arrays.
+ * int32 on the device, non-decreasing from 0 (row_off[n_groups] <= rows: rows behind the last group enter no
+ * result).  1..1024 groups, rows at most 2^31 - 4097; groups without rows get zeros.  Every product is exact in fp32;
+ * sums are held in fp32 and split over row chunks that are added in a fixed order.  An infinity or NaN of B reaches its own column,
+ * a block of X that holds one its own rows.  Offsets that break these rules give wrong values but no access outside
+ * the arrays.  Rows of q and B that start on multiples of four bytes are read fastest; rows of more than 256 KB may be
+ * refused (JANUS_EUNSUPPORTED).
  */
 int64_t janus_packed_wgrad_workspace(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type);
 int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t ldc, const void* B, int64_t ldb,

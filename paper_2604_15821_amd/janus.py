@@ -547,7 +547,7 @@ def _rows(t, name, dtype, shape, device):
         raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_cuda or t.device != device:
+    if device.index is None or t.get_device() != device.index:
         raise ValueError(f"{name}: on {t.device}, expected a device tensor on {device}")
     n, w = shape
     if n == 0 or w == 0:
@@ -564,7 +564,12 @@ def _rows(t, name, dtype, shape, device):
 
 def _param(t, name, d, device):
     """Address of an optional fp32 parameter vector of d values (None: NULL)."""
-    return None if t is None else _arg(t, name, "f32", (d,), device).data_ptr()
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.shape == (d,) and t.stride() == (1,) and \
+            t.get_device() == device.index:
+        return t.data_ptr()
+    return _arg(t, name, "f32", (d,), device).data_ptr()   # says what is wrong, or takes a vector of one value
 
 
 def _matrix(t, name):
