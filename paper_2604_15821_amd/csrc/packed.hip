@@ -6,6 +6,7 @@
 // stands for a block that held an infinity or NaN: all of it is NaN when read.
 // A power of two and seven bits fit bf16 exactly, so a product with a bf16 value is exact in fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.h"
 
@@ -474,25 +475,52 @@ __global__ __launch_bounds__(1024) void packed_chunks_kernel(const int* __restri
   if (g == 0) *n_chunks = min(all, most);
 }
 
-// Adds the partials of groups with several chunks, in order, four in flight.
+// The sum of partials [k0, k1) at p, in order, FLIGHT in flight.
+template <int FLIGHT, typename vec>
+__device__ __forceinline__ vec sum_partials(const float* __restrict__ p, long long PQ, int k0, int k1) {
+  vec v = {};
+  for (int k = k0; k < k1; k += FLIGHT) {
+    vec u[FLIGHT];
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j) u[j] = *reinterpret_cast<const vec*>(p + min(k + j, k1 - 1) * PQ);
+#pragma unroll
+    for (int j = 0; j < FLIGHT; ++j)
+      if (k + j < k1) v += u[j];
+  }
+  return v;
+}
+
+// Adds the partials of groups with several chunks.  A thread owns V neighbouring values; from eight chunks on, the
+// workgroup's four waves take a quarter of the chunks each for the same values, added in order.
+template <int V>
 __global__ __launch_bounds__(256) void packed_reduce_kernel(const float* __restrict__ partial,
                                                             const int* __restrict__ first,
                                                             const int* __restrict__ count, long long PQ,
                                                             float* __restrict__ G) {
+  typedef float vec __attribute__((ext_vector_type(V)));
+  __shared__ vec red[3][64];
   const int g = blockIdx.y, n = count[g];
   if (n < 2) return;
   const float* p = partial + first[g] * PQ;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < PQ; i += (long long)gridDim.x * 256) {
-    float v = 0.f;
-    for (int k = 0; k < n; k += 4) {
-      float u[4];
+  float* out = G + g * PQ;
+  if (n < 8) {
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * V; i < PQ; i += (long long)gridDim.x * 256 * V)
+      *reinterpret_cast<vec*>(out + i) = sum_partials<4, vec>(p + i, PQ, 0, n);
+    return;
+  }
+  const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, each = (n + 3) / 4;
+  for (long long i0 = (long long)blockIdx.x * (64 * V); i0 < PQ; i0 += (long long)gridDim.x * (64 * V)) {
+    const long long i = i0 + lane * V;
+    vec v = {};
+    if (i < PQ) v = sum_partials<8, vec>(p + i, PQ, slice * each, min((slice + 1) * each, n));
+    if (slice) red[slice - 1][lane] = v;
+    __syncthreads();
+    if (slice == 0 && i < PQ) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) u[j] = p[min(k + j, n - 1) * PQ + i];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (k + j < n) v += u[j];
+      for (int q = 0; q < 3; ++q) v += red[q][lane];
+      *reinterpret_cast<vec*>(out + i) = v;
     }
-    G[g * PQ + i] = v;
+    __syncthreads();
   }
 }
 
@@ -503,8 +531,8 @@ struct WgradPlan {
 // The chunk length.  Where at least half of the 512 resident workgroups are left after one more chunk per group (whose
 // last chunks are ragged), chunks that fill them in one round; else half of what each would get of all rows, so
 // that the last ones end together.  (One group of 65 536 rows, 512 x 2048, bf16: 227 us by the second rule, 185 by the first.)
-// Not below 512 rows, where partials cost more than they save (20 000 rows, one group, 256 x 256, fp32: 30 us at 512,
-// 38 at 256), nor above 16 384, so that a chunk's bytes stay within the 32-bit offsets of a buffer for rows of up to
+// Not below 512 rows, where partials cost more than they save (100 000 rows, 4 groups, 128 x 128, bf16: 29 us at 512,
+// 36 at 256), nor above 16 384, so that a chunk's bytes stay within the 32-bit offsets of a buffer for rows of up to
 // 256 KB.
 constexpr int kMostChunkRows = 16384, kWgSlots = 512;
 static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
@@ -630,8 +658,14 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
     else go(std::false_type{});
   });
   const int64_t PQ = (int64_t)P * Q;
-  if (rows > w.kc)   // else no group has several chunks
-    hipLaunchKernelGGL(packed_reduce_kernel, dim3(cdiv(PQ, 256) < 1024 ? cdiv(PQ, 256) : 1024, n_groups), dim3(256),
-                       0, st, partial, first, count, PQ, G);
+  if (rows > w.kc) {   // else no group has several chunks
+    auto reduce = [&](auto v) {
+      const unsigned bx = cdiv(PQ, 64 * v.value);
+      hipLaunchKernelGGL(packed_reduce_kernel<v.value>, dim3(bx < 1024 ? bx : 1024, n_groups), dim3(256), 0, st, partial,
+                         first, count, PQ, G);
+    };
+    if (PQ % 4 == 0 && rows_aligned(G, 0, 4)) reduce(std::integral_constant<int, 4>{});
+    else reduce(std::integral_constant<int, 1>{});
+  }
   return launched();
 }

@@ -189,6 +189,16 @@ def test_wgrad_many_groups(groups):
     _wgrad_check(p, b, off, janus.packed_wgrad(p, b.cuda(), off.cuda()), "bf16")
 
 
+@pytest.mark.parametrize("t", TYPES)
+def test_wgrad_many_chunks_of_odd_blocks(t):
+    """Groups of 18 and of 2 chunks whose gradients are no multiple of four values."""
+    from paper_2604_15821_amd import janus
+    banner("packed_wgrad odd blocks", t)
+    x, b, off = _wgrad_case(11, [9000, 700, 1], 33, 37, t)
+    p = janus.pack_rows(x.cuda())
+    _wgrad_check(p, b, off, janus.packed_wgrad(p, b.cuda(), off.cuda()), t)
+
+
 @pytest.mark.parametrize("rows,P,Q", [(9000, 300, 520), (4000, 1024, 1030), (1200, 2048, 64)])
 def test_wgrad_one_group(rows, P, Q):
     """Fewer chunks than dies, with many tiles each."""
