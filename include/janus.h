@@ -540,7 +540,7 @@ typedef enum janus_act { JANUS_ACT_NONE = 0, JANUS_ACT_SILU = 1 } janus_act;
  *   rows      rows of every array (>= 0, below 2^31)
  *   d         width, 1..8192 (wider: JANUS_EUNSUPPORTED)
  *   type      janus_type of x, b, r, n, the gate and their gradients
- *   eps       >= 0
+ *   eps       >= 0 (with 0, a row of zeros has no norm and gives NaN)
  *   w_post, scale, w_pre  [d] fp32, or NULL
  *   gate      NULL; [rows, d] (one gate per row) with gate_off NULL; or [n_seq, d], one
  *             gate per sequence (structure), with
@@ -596,7 +596,8 @@ int janus_residual_norm_grad(const janus_norm* p /* host */, const void* dr, int
  * x and y need rows that start on 16 bytes.  With 16-bit weights the hidden values enter the second product as two
  * bf16 each (to 2^-16 of themselves, in fp32's range).  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
  * [tokens, top_k] fp32; expert ids are always valid and distinct.  A token whose logits are all -inf gets
- * gates of zero and y = 0; one with a logit of NaN or +inf gets gates and y of NaN.  Neither reaches other tokens.
+ * gates of zero and y = 0 (an expert with a gate of zero is left out, whatever its weights hold); one with a
+ * logit of NaN or +inf gets gates and y of NaN.  Neither reaches other tokens.
  * The choice is exact up to the fp32 rounding of the logits.  y may not overlap x.
  * Errors: JANUS_EINVAL (also misaligned arrays), JANUS_EUNSUPPORTED (sizes beyond these), JANUS_EHIP.
  */
@@ -621,8 +622,9 @@ int janus_expert_layer(const janus_experts* p /* host */, const void* x, int64_t
  * Activations in 8 bits.  The columns of a row are cut into blocks of 32; a block holds int8
  * values q and one code byte c and stands for q 2^(c - 127).  The power of two is the least with
  * max|x| <= 127 2^(c - 127), but not below 2^-126; values are rounded to nearest, ties to even, so
- * each is off by at most max|x| / 127 of its block.  A block with an infinity or NaN gets c = 255
- * and q = 0 and reads as NaN.
+ * each is off by at most max|x| / 127 of its block (magnitudes from 63.5 2^122, 3.376e38, on round to 2^128 and read
+ * as infinity).  A block with an infinity or NaN gets c = 255 and q = 0 and reads as NaN; c = 0, which no block
+ * gets, reads as zeros.
  *   q [rows, d] int8, rows ldq apart;  code [rows, ceil(d / 32)] uint8, rows ldc apart.
  * Columns of q between d and ldq, and of code behind the last block, are neither read into a result nor written.
  */

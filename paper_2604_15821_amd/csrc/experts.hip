@@ -438,13 +438,14 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs
     if (find_slots(a, eid, s) == 0) return;
   }
   for (int base = 0; base < s.count; base += 16 * MT)
-    expert_product<T, T, Eight<T>, COLS, MT>(s, base, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d, a.d, deep_waves(a.d), lds,
-                                           [&](int t, int c, float v) {
-                                             hidden[(long long)s.slot[t] * a.h + c] = silu(v);
-                                           });
+    expert_product<T, T, Eight<T>, COLS, MT>(s, base, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d,
+                                             a.d, deep_waves(a.d), lds, [&](int t, int c, float v) {
+                                               hidden[(long long)s.slot[t] * a.h + c] = silu(v);
+                                             });
 }
 
-// y[t, c] = sum_q gate[t, q] sum_z part[t k + q, z, c] in that order, eight parts in flight.
+// y[t, c] = sum_q gate[t, q] sum_z part[t k + q, z, c] in that order, eight parts in flight.  A gate of zero leaves its
+// expert out, whatever that one's weights hold.
 template <typename F>
 __device__ __forceinline__ float expert_sum(const ExpertArgs& a, const float* __restrict__ gate, float* part, int splits,
                                             int t, int c, F load) {
@@ -460,7 +461,11 @@ __device__ __forceinline__ float expert_sum(const ExpertArgs& a, const float* __
     for (int j = 0; j < 8; ++j)
       if (i + j < n) {
         v += u[j];
-        if ((i + j + 1) % splits == 0) out += g[(i + j) / splits] * v, v = 0.f;
+        if ((i + j + 1) % splits == 0) {
+          const float w = g[(i + j) / splits];
+          out += w == 0.f ? 0.f : w * v;
+          v = 0.f;
+        }
       }
   }
   return out;

@@ -136,7 +136,15 @@ def test_masked_experts_and_masked_tokens():
     s["beta"] = torch.full((6,), torch.finfo(torch.float32).min)
     got = _run(s, 2)
     assert torch.isfinite(got[0]).all() and (got[2] == 1 / 6).all()   # x router vanishes next to it
-    # a masked expert's weights are not used
+    # a masked expert's weights are not used, also where it fills up the top_k
+    s["beta"] = torch.full((6,), -float("inf"))
+    s["beta"][4] = 0.0
+    clean = _run(s, 3)
+    for e in (0, 1, 2, 3, 5):
+        s["w_up"][e] = float("nan")
+        s["w_down"][e] = float("inf")
+    assert torch.equal(_run(s, 3)[0], clean[0])
+    s = _case(2, 9, 64, 128, 6, "f32")
     s["beta"] = torch.zeros(6)
     s["beta"][1] = -float("inf")
     s["w_up"][1] = float("nan")
