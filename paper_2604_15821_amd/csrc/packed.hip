@@ -644,7 +644,7 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
   int* count = reinterpret_cast<int*>(base + w.count);
   float* partial = reinterpret_cast<float*>(base + w.partial);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(packed_chunks_kernel, dim3(1), dim3(1024), 0, st, row_off, n_groups, rows, w.kc, chunks, w.most,
+  hipLaunchKernelGGL(packed_chunks_kernel, dim3(1), dim3((n_groups + 63) / 64 * 64), 0, st, row_off, n_groups, rows, w.kc, chunks, w.most,
                      n_chunks, first, count);
   const bool words = rows_aligned(q, ldq, 1, 4) && rows_aligned(B, ldb, type_bytes(type), 4);
   with_type(type, [&](auto zero) {
