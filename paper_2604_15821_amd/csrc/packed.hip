@@ -411,13 +411,13 @@ __global__ __launch_bounds__(256, 2) void packed_wgrad_kernel(const int8_t* __re
   };
   if (steps > 0) {
     load(r0);
+    load(r1);
     stage(r0, lds);
-    load(r0);
     __syncthreads();
   }
   for (int s = 0; s < steps; s += 2) {
-    step(lds, lds + kStage, r0, r1);
-    if (s + 1 < steps) step(lds + kStage, lds, r1, r0);
+    step(lds, lds + kStage, r1, r0);
+    if (s + 1 < steps) step(lds + kStage, lds, r0, r1);
   }
 
   float* out = ch.alone ? G + (long long)ch.group * P * Q : partial + (long long)at * P * Q;
