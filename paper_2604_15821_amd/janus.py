@@ -580,29 +580,23 @@ def _matrix(t, name):
     return t.shape[0], t.shape[1], t.device
 
 
-class _on:
-    """The device of the tensors is current within (a switch only where it is not yet); gives its
-    current stream, on which the call runs."""
-
-    def __init__(self, device):
-        self.device, self.guard = device, None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-        # the handle itself: current_stream() builds an object around it, 3 us of a call of 12
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
-
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
-
-
 def _call(rc, where):
     if rc < 0:
         raise JanusError(rc, where)
     return rc
+
+
+def _launch(device, where, call, *args):
+    """The library call on the current stream of the tensors' device, which is made the current one where it is not."""
+    # the stream's handle itself: current_stream() builds an object around it, 3 us of a call of 12
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        rc = call(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, stream)
+    if rc < 0:
+        raise JanusError(rc, where)
 
 
 def _norm(rows, d, like, device, w_post, gate, gate_off, scale, w_pre, eps):
@@ -647,8 +641,7 @@ def residual_norm(x, b, w_post=None, gate=None, gate_off=None, scale=None, w_pre
             raise ValueError("out: n is given exactly where w_pre is")
     pr, ldr = _rows(r, "r", b.dtype, (rows, d), dev)
     pn, ldn = (None, 0) if n is None else _rows(n, "n", b.dtype, (rows, d), dev)
-    with _on(dev) as stream:
-        _call(_lib().janus_residual_norm(C.byref(p), px, ldx, pb, ldb, pr, ldr, pn, ldn, stream), "janus_residual_norm")
+    _launch(dev, "janus_residual_norm", _lib().janus_residual_norm, C.byref(p), px, ldx, pb, ldb, pr, ldr, pn, ldn)
     return r, n
 
 
@@ -691,12 +684,23 @@ def residual_norm_grad(dr, dn, r, b, w_post=None, gate=None, gate_off=None, scal
     adr = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
     lib = _lib()
     size = _call(lib.janus_residual_norm_grad_workspace(C.byref(p)), "janus_residual_norm_grad_workspace")
-    with _on(dev) as stream:
-        work = torch.empty(size, dtype=torch.uint8, device=dev)
-        _call(lib.janus_residual_norm_grad(C.byref(p), pdr, lddr, pdn, lddn, pr, ldr, pb, ldb, pdx, lddx, pdb, lddb,
-                                           adr(dw_post), adr(dscale), adr(dw_pre), adr(dgate), d, work.data_ptr(), size,
-                                           stream), "janus_residual_norm_grad")
+    work = torch.empty(size, dtype=torch.uint8, device=dev)
+    _launch(dev, "janus_residual_norm_grad", lib.janus_residual_norm_grad, C.byref(p), pdr, lddr, pdn, lddn, pr, ldr, pb,
+            ldb, pdx, lddx, pdb, lddb, adr(dw_post), adr(dscale), adr(dw_pre), adr(dgate), d, work.data_ptr(), size)
     return NormGrads(dx, db, dw_post, dgate, dscale, dw_pre)
+
+
+def _weights(t, name, dtype, shape, device):
+    """Address of a contiguous weight tensor."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    if device.index is None or t.get_device() != device.index or not t.is_contiguous():
+        raise ValueError(f"{name}: must be a contiguous tensor on {device}")
+    return t.data_ptr()
 
 
 def expert_layer(x, router, w_up, w_down, top_k, beta=None, normalize=False, out=None):
@@ -712,28 +716,19 @@ def expert_layer(x, router, w_up, w_down, top_k, beta=None, normalize=False, out
     n, _, h = w_up.shape
     code = _type_of(x, "x")
     px, ldx = _rows(x, "x", x.dtype, (tokens, d), dev)
-    _arg(router, "router", "f32", (d, n), dev)
-    for name, t, shape in (("w_up", w_up, (n, d, h)), ("w_down", w_down, (n, h, d))):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
-        if t.dtype != x.dtype:
-            raise TypeError(f"{name}: dtype {t.dtype}, expected {x.dtype}")
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
-        if t.device != dev or not t.is_contiguous():
-            raise ValueError(f"{name}: must be a contiguous tensor on {dev}")
-    p = Experts(d, h, n, int(top_k), code, int(bool(normalize)), router.data_ptr(), _param(beta, "beta", n, dev),
-                w_up.data_ptr(), w_down.data_ptr())
+    pr = _weights(router, "router", torch.float32, (d, n), dev)
+    pu = _weights(w_up, "w_up", x.dtype, (n, d, h), dev)
+    pw = _weights(w_down, "w_down", x.dtype, (n, h, d), dev)
+    p = Experts(d, h, n, int(top_k), code, int(bool(normalize)), pr, _param(beta, "beta", n, dev), pu, pw)
     lib = _lib()
     size = _call(lib.janus_expert_layer_workspace(C.byref(p), tokens), "janus_expert_layer_workspace")
     y = torch.empty(tokens, d, dtype=x.dtype, device=dev) if out is None else out
     py, ldy = _rows(y, "out", x.dtype, (tokens, d), dev)
     eid = torch.empty(tokens, p.top_k, dtype=torch.int32, device=dev)
     gate = torch.empty(tokens, p.top_k, dtype=torch.float32, device=dev)
-    with _on(dev) as stream:
-        work = torch.empty(size, dtype=torch.uint8, device=dev)
-        _call(lib.janus_expert_layer(C.byref(p), px, ldx, tokens, py, ldy, eid.data_ptr(), gate.data_ptr(),
-                                     work.data_ptr(), size, stream), "janus_expert_layer")
+    work = torch.empty(size, dtype=torch.uint8, device=dev)
+    _launch(dev, "janus_expert_layer", lib.janus_expert_layer, C.byref(p), px, ldx, tokens, py, ldy, eid.data_ptr(),
+            gate.data_ptr(), work.data_ptr(), size)
     return y, eid, gate
 
 
@@ -760,13 +755,15 @@ def pack_rows(x, out=None) -> PackedRows:
     code = _type_of(x, "x")
     px, ldx = _rows(x, "x", x.dtype, (rows, d), dev)
     if out is None:
-        out = PackedRows(torch.empty(rows, (d + 15) // 16 * 16, dtype=torch.int8, device=dev)[:, :d],
-                         torch.empty(rows, (d + 31) // 32, dtype=torch.uint8, device=dev))
-    n, w, _, at = _packed(out, dev)
-    if (n, w) != (rows, d):
-        raise ValueError(f"out: {n} x {w}, expected {rows} x {d}")
-    with _on(dev) as stream:
-        _call(_lib().janus_pack_rows(px, ldx, code, rows, d, *at, stream), "janus_pack_rows")
+        wide = (d + 15) // 16 * 16
+        q = torch.empty(rows, wide, dtype=torch.int8, device=dev)
+        out = PackedRows(q if wide == d else q[:, :d], torch.empty(rows, (d + 31) // 32, dtype=torch.uint8, device=dev))
+        at = (q.data_ptr(), wide, out.code.data_ptr(), (d + 31) // 32)
+    else:
+        n, w, _, at = _packed(out, dev)
+        if (n, w) != (rows, d):
+            raise ValueError(f"out: {n} x {w}, expected {rows} x {d}")
+    _launch(dev, "janus_pack_rows", _lib().janus_pack_rows, px, ldx, code, rows, d, *at)
     return out
 
 
@@ -789,9 +786,7 @@ def unpack_rows(packed, dtype, act="none", grad=None, value=None, out=None):
     ps, lds = (None, 0) if second is None else _rows(second, "value", dtype, (rows, d), dev)
     if grad is None:
         ps, lds, pf, ldf = pf, ldf, None, 0
-    with _on(dev) as stream:
-        _call(_lib().janus_unpack_rows(*at, rows, d, code, ACT[act], pg, ldg, pf, ldf, ps, lds, stream),
-              "janus_unpack_rows")
+    _launch(dev, "janus_unpack_rows", _lib().janus_unpack_rows, *at, rows, d, code, ACT[act], pg, ldg, pf, ldf, ps, lds)
     return first if second is None else (first, second)
 
 
@@ -807,13 +802,13 @@ def packed_wgrad(packed, B, row_off, out=None):
     G = row_off.shape[0] - 1
     if out is None:
         out = torch.empty(max(G, 0), P, Q, dtype=torch.float32, device=dev)
-    _arg(out, "out", "f32", (G, P, Q), dev)
+    else:
+        _arg(out, "out", "f32", (G, P, Q), dev)
     lib = _lib()
     size = _call(lib.janus_packed_wgrad_workspace(rows, G, P, Q, code), "janus_packed_wgrad_workspace")
-    with _on(dev) as stream:
-        work = torch.empty(size, dtype=torch.uint8, device=dev)
-        _call(lib.janus_packed_wgrad(*at, pb, ldb, code, out.data_ptr(), row_off.data_ptr(), G, rows, P, Q,
-                                     work.data_ptr(), size, stream), "janus_packed_wgrad")
+    work = torch.empty(size, dtype=torch.uint8, device=dev)
+    _launch(dev, "janus_packed_wgrad", lib.janus_packed_wgrad, *at, pb, ldb, code, out.data_ptr(), row_off.data_ptr(), G,
+            rows, P, Q, work.data_ptr(), size)
     return out
 
 
