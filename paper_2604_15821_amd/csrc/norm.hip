@@ -15,7 +15,9 @@
 //
 // so one column sum serves scale and w_post, and the statistics are taken again from r and b, which
 // are read anyway: nothing but r and b need be kept for the backward pass.  All of it is bound by
-// memory: 2 rows in and 2 out, backwards 4 in and 2 out.
+// memory: 2 rows in and 2 out, backwards 4 in and 2 out.  Measured: 59 186 x 512 fp32, 512 sequences, 100 us
+// forward (4.9 TB/s, where a copy reaches 5.2), 157 us backward (4.7 TB/s) and 10 us for its sums; 16 384 x 4096 bf16
+// 170 and 8 us.
 //
 // Work: a group of L lanes owns a row and C of its columns per lane; groups take runs of
 // consecutive rows, so that the parameters, a sequence's gate and the column sums stay in
