@@ -118,6 +118,10 @@ def test_packed_wgrad_arrays():
         bad = list(good)
         bad[k] = v
         assert lib.janus_packed_wgrad(*bad, None) == EINVAL, (k, v)
+    for k in (1, 5):   # rows too far apart for the 32-bit offsets of a chunk
+        bad = list(good)
+        bad[k] = 1 << 30
+        assert lib.janus_packed_wgrad(*bad, None) == EUNSUP, k
     for bad in ((-1, 2, 40, 24, 0), (4, 0, 40, 24, 0), (4, 1025, 40, 24, 0), (4, 2, 0, 24, 0), (4, 2, 40, 0, 0), (4, 2, 40, 24, 3)):
         assert lib.janus_packed_wgrad_workspace(*bad) == EINVAL
 

@@ -177,3 +177,72 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Rows 2^26 values apart, 35 of them: byte and element offsets past 2^31."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("block large offsets: norm, pack, unpack")
+    rows, d, ld = 35, 72, 1 << 26
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    small = torch.randn(rows, d, generator=g, device="cuda:0").bfloat16()
+    wide = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda:0")
+    x = wide.as_strided((rows, d), (ld, 1))
+    x.copy_(small)
+    b, w = torch.randn(rows, d, generator=g, device="cuda:0").bfloat16(), torch.rand(d, generator=g, device="cuda:0")
+    want = janus.residual_norm(small, b, w_post=w, w_pre=w)
+    got = janus.residual_norm(x, b, w_post=w, w_pre=w, out=(x, torch.empty_like(b)))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    back = janus.residual_norm_grad(small, b, x, b, w_post=w, w_pre=w)
+    ref = janus.residual_norm_grad(small, b, want[0], b, w_post=w, w_pre=w)
+    assert all(torch.equal(p, q) for p, q in zip(back, ref) if q is not None)
+    q = torch.empty(rows * ld, dtype=torch.int8, device="cuda:0").as_strided((rows, d), (ld, 1))
+    code = torch.empty(rows, 3, dtype=torch.uint8, device="cuda:0")
+    p = janus.pack_rows(x, out=janus.PackedRows(q, code))
+    ref = janus.pack_rows(want[0])
+    assert torch.equal(p.q, ref.q) and torch.equal(p.code, ref.code)
+    assert torch.equal(janus.unpack_rows(p, torch.bfloat16, act="silu", grad=x, out=x),
+                       janus.unpack_rows(ref, torch.bfloat16, act="silu", grad=want[0]))
+
+
+def test_weight_gradient_beyond_32_bit_offsets():
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("block large offsets: weight gradient")
+    rows, P, Q, ld = 60_000, 40, 24, 40_000
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    small = torch.randn(rows, Q, generator=g, device="cuda:0").bfloat16()
+    B = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda:0").as_strided((rows, Q), (ld, 1))
+    B.copy_(small)
+    p = janus.pack_rows(torch.randn(rows, P, generator=g, device="cuda:0"))
+    off = torch.tensor([0, 1000, rows - 7, rows], dtype=torch.int32, device="cuda:0")
+    out = torch.full((3, P, Q), float("nan"), device="cuda:0")
+    assert janus.packed_wgrad(p, B, off, out=out) is out
+    assert torch.equal(out, janus.packed_wgrad(p, small, off))
+
+
+def test_expert_weights_beyond_32_bit_offsets():
+    """The last of 17 experts begins past 2^31 values; only its weights are filled."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("block large offsets: expert layer")
+    n, d, h, tokens = 17, 2048, 65_536, 3
+    g = torch.Generator(device="cuda:0").manual_seed(5)
+    up = torch.empty(n, d, h, dtype=torch.bfloat16, device="cuda:0")
+    down = torch.empty(n, h, d, dtype=torch.bfloat16, device="cuda:0")
+    up[16] = torch.randn(d, h, generator=g, device="cuda:0") / d ** 0.5
+    down[16] = torch.randn(h, d, generator=g, device="cuda:0") / h ** 0.5
+    x = torch.randn(tokens, d, generator=g, device="cuda:0").bfloat16()
+    beta = torch.full((n,), -float("inf"), device="cuda:0")
+    beta[16] = 0.0
+    y, eid, gate = janus.expert_layer(x, torch.zeros(d, n, device="cuda:0"), up, down, 1, beta=beta)
+    assert (eid == 16).all() and (gate == 1).all()
+    a = x.float() @ up[16].float()
+    s = a * torch.sigmoid(a)
+    want = s.double().cpu() @ down[16].cpu().double()
+    size = s.abs().double().cpu() @ down[16].cpu().double().abs()
+    # fp32 pre-activations on both sides (2 (d + 8) e of their magnitudes, of the order of sqrt(d) times the value), the
+    # hidden values to 2^-16, the sum of h products, and the rounding to bf16
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -16 + 2 * (h + 8) * E + 4 * (d + 8) * E) * size
+    assert ((y.cpu().double() - want).abs() <= tol).all()

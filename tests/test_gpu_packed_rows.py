@@ -71,6 +71,8 @@ def test_pack_and_unpack_are_exact(rows, d, t):
     for out in TYPES:
         got = janus.unpack_rows(p, _dt(out))
         assert torch.equal(got.cpu(), want.to(_dt(out)))
+        into = torch.empty_like(got)
+        assert janus.unpack_rows(p, _dt(out), out=into) is into and torch.equal(into, got)
 
 
 def test_pack_keeps_strides_and_the_columns_between():
