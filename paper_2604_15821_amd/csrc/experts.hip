@@ -26,13 +26,13 @@ struct ExpertArgs {
 
 // Router of one token by a workgroup of W waves.  Lanes take V neighbouring experts each (four, of which the last
 // lane's may be its neighbour's too; one where there are fewer), the rest of a wave and the waves take rows, up to
-// sixteen in flight; rows are added over the lanes and then over the waves.  Every expert then counts
+// sixteen in flight; rows are added over the lanes (to four sums per wave) and then over the waves.  Every expert then counts
 // those that come before it: its rank is its place among the chosen, without a round for each of them.
 // NaN ranks like -inf and makes the token's gates NaN; a token without any finite or +inf logit
 // (all experts masked) has gates of zero.
 template <int W>
 struct RouteArea {
-  float red[W][kMaxExperts];
+  float red[W][kMaxExperts];   // of a wave: one sum per expert, or up to four one behind the other
   __align__(16) float key[kMaxExperts];
   float sum[4], top[kMaxTopK], gate[kMaxTopK];
   int eid[kMaxTopK], nan;
@@ -73,51 +73,63 @@ __device__ __forceinline__ void route_sums(const ExpertArgs& a, const T* __restr
         i += 8 * rows;
       }
     }
+    const int left = max(wide, 16);   // lanes of one sum: four, two or one sums per wave
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      for (int o = wide; o < 64; o <<= 1) sum[c] += __shfl_xor(sum[c], o, 64);
-      if (lane < wide && u < units) s.red[wave][c0 + c] = sum[c];
+      for (int o = wide; o < left; o <<= 1) sum[c] += __shfl_xor(sum[c], o, 64);
+      if ((lane & (left - 1)) < wide && u < units) s.red[wave][lane / left * (V * left) + c0 + c] = sum[c];
     }
   }
   __syncthreads();
 }
-template <int W>
-__device__ __forceinline__ float route_sum(const RouteArea<W>& s, int e) {
+template <int V, int W>
+__device__ __forceinline__ float route_sum(const RouteArea<W>& s, int n, int e) {
+  const int left = n <= 16 * V ? 16 : n <= 32 * V ? 32 : 64;
   float l = 0.f;
+  for (int i = 0; i < 64 / left; ++i) {
 #pragma unroll
-  for (int p = 0; p < W; ++p) l += s.red[p][e];
+    for (int p = 0; p < W; ++p) l += s.red[p][i * (V * left) + e];
+  }
   return l;
 }
 
-// The choice from the logit l of expert threadIdx.x, before beta.
+// beta of expert threadIdx.x, asked for before the sums so that it is there after them
+__device__ __forceinline__ float route_beta(const ExpertArgs& a) {
+  return a.beta && (int)threadIdx.x < a.n ? a.beta[threadIdx.x] : 0.f;
+}
+
+// The chosen experts (eid) and their logits (top) from the logit l of expert threadIdx.x.
 template <int W>
-__device__ __forceinline__ void route_choose(const ExpertArgs& a, float l, RouteArea<W>& s) {
-  const int e = threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void route_rank(const ExpertArgs& a, float l, RouteArea<W>& s) {
+  const int e = threadIdx.x;
   if (e == 0) s.nan = 0;
-  __syncthreads();
-  float key = -INFINITY;
-  if (e < a.n) {
-    if (a.beta) l += a.beta[e];
-    if (l == l) key = l;
-    else s.nan = 1;
-  } else {
-    l = -INFINITY;
-  }
+  const float key = e < a.n && l == l ? l : -INFINITY;
   if (e < kMaxExperts) s.key[e] = key;
   __syncthreads();
-  int rank = 0;
   if (e < a.n) {
-    for (int q = 0; q < a.n; q += 4) {   // keys past the last expert are -inf and of a higher index
-      const f32x4 o = *reinterpret_cast<const f32x4*>(s.key + q);
+    if (l != l) s.nan = 1;
+    int rank = 0;
+    for (int q = 0; q < a.n; q += 32) {   // keys past the last expert are -inf and of a higher index
+      f32x4 o[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) rank += o[j] > key || (o[j] == key && q + j < e);
+      for (int i = 0; i < 8; ++i) o[i] = *reinterpret_cast<const f32x4*>(s.key + q + 4 * i);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rank += q + 4 * i + j < e ? o[i][j] >= key : o[i][j] > key;
     }
     if (rank < a.k) s.top[rank] = key, s.eid[rank] = e;
   }
   __syncthreads();
+}
+
+// The gates of the choice.
+template <int W>
+__device__ __forceinline__ void route_gates(const ExpertArgs& a, float l, RouteArea<W>& s) {
+  const int e = threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float top = s.top[0];
   if (e < kMaxExperts) {
-    const float p = wave_sum(top == -INFINITY ? 0.f : expf(l - top));
+    const float p = wave_sum(top == -INFINITY || e >= a.n ? 0.f : expf(l - top));
     if (lane == 0) s.sum[wave] = p;
   }
   __syncthreads();
@@ -133,12 +145,6 @@ __device__ __forceinline__ void route_choose(const ExpertArgs& a, float l, Route
   __syncthreads();
 }
 
-template <typename T, int V, int W>
-__device__ __forceinline__ void route_token(const ExpertArgs& a, const T* __restrict__ x, RouteArea<W>& s) {
-  route_sums<T, V, W>(a, x, 0, a.d, s);
-  route_choose(a, (int)threadIdx.x < a.n ? route_sum(s, threadIdx.x) : 0.f, s);
-}
-
 constexpr int kRouteWaves = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(64 * kRouteWaves) void expert_route_kernel(ExpertArgs a, const T* __restrict__ x,
@@ -149,7 +155,11 @@ __global__ __launch_bounds__(64 * kRouteWaves) void expert_route_kernel(ExpertAr
   const int t = blockIdx.x;
   if (t == 0)   // the counts of the second product's workgroups
     for (int i = threadIdx.x; i < n_arrived; i += 64 * kRouteWaves) arrived[i] = 0;
-  route_token<T, V, kRouteWaves>(a, x + t * ldx, s);
+  const float beta = route_beta(a);
+  route_sums<T, V, kRouteWaves>(a, x + t * ldx, 0, a.d, s);
+  const float l = (int)threadIdx.x < a.n ? route_sum<V>(s, a.n, threadIdx.x) + beta : 0.f;
+  route_rank(a, l, s);
+  route_gates(a, l, s);
   if ((int)threadIdx.x < a.k) {
     eid[t * a.k + threadIdx.x] = s.eid[threadIdx.x];
     gate[t * a.k + threadIdx.x] = s.gate[threadIdx.x];
@@ -166,7 +176,7 @@ __global__ __launch_bounds__(64 * kRouteWaves) void expert_logits_kernel(ExpertA
   const int t = blockIdx.y, begin = blockIdx.x * rows;
   route_sums<T, V, kRouteWaves>(a, x + t * ldx, begin, min(begin + rows, a.d), s);
   const int e = threadIdx.x;
-  if (e < a.n) share[((long long)t * gridDim.x + blockIdx.x) * a.n + e] = route_sum(s, e);
+  if (e < a.n) share[((long long)t * gridDim.x + blockIdx.x) * a.n + e] = route_sum<V>(s, a.n, e);
 }
 __global__ __launch_bounds__(kMaxExperts) void expert_choose_kernel(ExpertArgs a, const float* __restrict__ share,
                                                                     int shares, int* __restrict__ eid,
@@ -177,6 +187,7 @@ __global__ __launch_bounds__(kMaxExperts) void expert_choose_kernel(ExpertArgs a
   if (t == 0)
     for (int i = e; i < n_arrived; i += kMaxExperts) arrived[i] = 0;
   float l = 0.f;
+  const float beta = route_beta(a);
   if (e < a.n) {
     const float* p = share + (long long)t * shares * a.n + e;
     float v[kMostShares];
@@ -185,8 +196,10 @@ __global__ __launch_bounds__(kMaxExperts) void expert_choose_kernel(ExpertArgs a
 #pragma unroll
     for (int z = 0; z < kMostShares; ++z)
       if (z < shares) l += v[z];
+    l += beta;
   }
-  route_choose(a, l, s);
+  route_rank(a, l, s);
+  route_gates(a, l, s);
   if (e < a.k) eid[t * a.k + e] = s.eid[e], gate[t * a.k + e] = s.gate[e];
 }
 
@@ -428,13 +441,13 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs
                                                                       float* __restrict__ hidden) {
   __shared__ ExpertSlots s;
   __shared__ float lds[kExpertWaves * 256 * COLS];
+  __shared__ std::conditional_t<kRoute, RouteArea<kExpertWaves>, int> r;
+  float l = 0.f;
   if constexpr (kRoute) {
-    __shared__ RouteArea<kExpertWaves> r;
-    route_token<T, V, kExpertWaves>(a, x, r);
-    if (blockIdx.x == 0 && blockIdx.y == 0) {
-      for (int i = threadIdx.x; i < n_arrived; i += 64 * kExpertWaves) arrived[i] = 0;
-      if ((int)threadIdx.x < a.k) eid[threadIdx.x] = r.eid[threadIdx.x], gate[threadIdx.x] = r.gate[threadIdx.x];
-    }
+    const float beta = route_beta(a);
+    route_sums<T, V, kExpertWaves>(a, x, 0, a.d, r);
+    if ((int)threadIdx.x < a.n) l = route_sum<V>(r, a.n, threadIdx.x) + beta;
+    route_rank(a, l, r);
     if (threadIdx.x == 0) s.count = 1, s.slot[0] = blockIdx.y, s.expert = r.eid[blockIdx.y];
     __syncthreads();
   } else {
@@ -445,6 +458,13 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs
                                              a.d, deep_waves(a.d), lds, [&](int t, int c, float v) {
                                                hidden[(long long)s.slot[t] * a.h + c] = silu(v);
                                              });
+  if constexpr (kRoute) {   // the gates are not needed before
+    if (blockIdx.x == 0 && blockIdx.y == 0) {
+      route_gates(a, l, r);
+      for (int i = threadIdx.x; i < n_arrived; i += 64 * kExpertWaves) arrived[i] = 0;
+      if ((int)threadIdx.x < a.k) eid[threadIdx.x] = r.eid[threadIdx.x], gate[threadIdx.x] = r.gate[threadIdx.x];
+    }
+  }
 }
 
 // y[t, c] = sum_q gate[t, q] sum_z part[t k + q, z, c] in that order, eight parts in flight.  A gate of zero leaves its
