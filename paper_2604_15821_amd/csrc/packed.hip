@@ -553,9 +553,11 @@ static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
   w.first = w.chunks + (int64_t)w.most * sizeof(PackedChunk);
   w.count = w.first + 4 * (int64_t)groups;
   w.partial = (w.count + 4 * (int64_t)groups + 15) / 16 * 16;
-  w.total = w.partial + 4 * (int64_t)w.most * P * Q;
+  w.total = w.partial + (int64_t)(4ull * w.most * P * Q);   // sizes beyond a launch, which overflow it, are refused
   return w;
 }
+// Workgroups of the product: every die's share of the chunks, rounded up.
+static double wgrad_blocks(const WgradPlan& w) { return (w.most + 7) / 8 * 8.0 * w.tiles_p * w.tiles_q; }
 
 static PackShape pack_shape(long long rows, int d) {
   int tpr = 4;
@@ -619,7 +621,9 @@ extern "C" int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* co
 static int check_packed_wgrad(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type) {
   if (rows < 0 || rows > INT_MAX - 4096 || n_groups < 1 || n_groups > 1024 || P < 1 || Q < 1 || !type_known(type))
     return JANUS_EINVAL;
-  return JANUS_OK;
+  // a launch holds fewer than 2^32 threads
+  const WgradPlan w = wgrad_plan(rows, n_groups, P, Q, type);
+  return wgrad_blocks(w) < (1 << 24) ? JANUS_OK : JANUS_EUNSUPPORTED;
 }
 
 extern "C" int64_t janus_packed_wgrad_workspace(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type) {
@@ -638,9 +642,9 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
       work_bytes < janus_packed_wgrad_workspace(rows, n_groups, P, Q, type))
     return JANUS_EINVAL;
   const WgradPlan w = wgrad_plan(rows, n_groups, P, Q, type);
-  const int64_t blocks = ((int64_t)w.most + 7) / 8 * 8 * w.tiles_p * w.tiles_q;
+  const int64_t blocks = (int64_t)wgrad_blocks(w);
   const int64_t row_bytes = std::max({ldq, ldc, ldb * type_bytes(type)});
-  if (blocks > INT_MAX || (rows > 0 && row_bytes > (int64_t)UINT_MAX / (w.kc + 4 * kWgRows))) return JANUS_EUNSUPPORTED;
+  if (rows > 0 && row_bytes > (int64_t)UINT_MAX / (w.kc + 4 * kWgRows)) return JANUS_EUNSUPPORTED;
   char* base = static_cast<char*>(work);
   int* n_chunks = reinterpret_cast<int*>(base);
   PackedChunk* chunks = reinterpret_cast<PackedChunk*>(base + w.chunks);

@@ -126,6 +126,16 @@ def test_packed_wgrad_arrays():
         assert lib.janus_packed_wgrad_workspace(*bad) == EINVAL
 
 
+def test_packed_wgrad_sizes_beyond_a_launch():
+    lib = janus._lib()
+    most = 1 << 21   # 2^14 tiles of 128 rows x 1024 groups: 2^24 workgroups, 2^32 threads
+    for p_, q_ in ((most, 1), (1, 2 * most), ((1 << 31) - 1, (1 << 31) - 1)):
+        assert lib.janus_packed_wgrad_workspace(10, 1024, p_, q_, 1) == EUNSUP, (p_, q_)
+        bad = [P, p_, P, p_ // 32 + 1, P, q_, 1, P, P, 1024, 10, p_, q_, P, 1 << 62]
+        assert lib.janus_packed_wgrad(*bad, None) == EUNSUP, (p_, q_)
+    assert lib.janus_packed_wgrad_workspace(10, 1000, most, 1, 1) > 0
+
+
 def test_binding_refuses_before_the_library():
     x = torch.zeros(4, 64)
     for call in (lambda: janus.residual_norm(x, x), lambda: janus.residual_norm_grad(x, None, None, x),
