@@ -6,7 +6,7 @@
 // stands for a block that held an infinity or NaN: all of it is NaN when read.
 // A power of two and seven bits fit bf16 exactly, so a product with a bf16 value is exact in fp32.
 // Packing and unpacking are bound by memory: 150 001 x 2048 fp32 to 8 bits 316 us (4.9 TB/s); SiLU and the gradient
-// through it in bf16 400 us (5.4 TB/s).
+// through it in bf16 385 us (5.6 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -24,21 +24,34 @@ __device__ __forceinline__ int pack_code(float top) {
 // 2^(c - 127), NaN for 255
 __device__ __forceinline__ float code_scale(int c) { return __int_as_float(c == 255 ? 0x7FC00000 : c << 23); }
 
-// Eight columns of a row from column c, zero past d.
-template <typename T>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int c, int d, float (&v)[8]) {
-  if (c + 8 <= d) {
-    load_run<T, 8>(row + c, v);
-  } else {
+// Eight columns of a row from column c, and their values later, so that several arrays can be asked for before the
+// first is waited for.  Columns past d read the last one; WHOLE: d is a multiple of eight, there are none.
+template <typename T, bool WHOLE>
+struct Raw8 {
+  typedef unsigned words __attribute__((ext_vector_type(sizeof(T) < 2 ? 2 : 4), aligned(sizeof(T))));
+  static constexpr int kWords = sizeof(T) * 8 / sizeof(words);
+  words w[kWords];
+  __device__ __forceinline__ void load(const T* __restrict__ row, int c, int d) {
+    if (WHOLE || c + 8 <= d) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)row[min(c + j, d - 1)];   // all at once, then cut off
+      for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const words*>(row + c)[i];
+    } else {
+      T v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < d ? v[j] : 0.f;
+      for (int j = 0; j < 8; ++j) v[j] = row[min(c + j, d - 1)];
+      __builtin_memcpy(w, v, sizeof v);
+    }
   }
-}
-template <typename T>
+  __device__ __forceinline__ void values(float (&o)[8]) const {
+    T v[8];
+    __builtin_memcpy(v, w, sizeof v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (float)v[j];
+  }
+};
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void store8(T* __restrict__ row, int c, int d, const float (&v)[8]) {
-  if (c + 8 <= d) {
+  if (WHOLE || c + 8 <= d) {
     store_run<T, 8>(row + c, v);
   } else {
 #pragma unroll
@@ -63,8 +76,14 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackShape s, const T* __
   const int cols = (s.d + kPackBlock - 1) / kPackBlock * kPackBlock;
   for (long long m = (long long)blockIdx.x * per + threadIdx.x / s.tpr; m < s.rows; m += (long long)gridDim.x * per) {
     for (int c = t * 8; c < cols; c += s.tpr * 8) {
+      Raw8<T, false> raw;
+      raw.load(x + m * ldx, c, s.d);
       float v[8], top = 0.f;
-      load8(x + m * ldx, c, s.d, v);
+      raw.values(v);
+      if (c + 8 > s.d) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < s.d ? v[j] : 0.f;
+      }
       int bad = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -95,8 +114,9 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackShape s, const T* __
   }
 }
 
-// value = x, or SiLU(x) and out = grad SiLU'(x), of the stored x.
-template <typename T, bool kSilu>
+// value = x, or SiLU(x) and out = grad SiLU'(x), of the stored x.  Widths that are multiples of eight have no code for a
+// row's end, so that all loads of a thread are in flight together.
+template <typename T, bool kSilu, bool WHOLE>
 __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int8_t* __restrict__ q, long long ldq,
                                                           const uint8_t* __restrict__ code, long long ldc,
                                                           const T* grad, long long ldg, T* out, long long ldo, T* value,
@@ -104,23 +124,30 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
   const int per = 256 / s.tpr, t = threadIdx.x % s.tpr;
   for (long long m = (long long)blockIdx.x * per + threadIdx.x / s.tpr; m < s.rows; m += (long long)gridDim.x * per) {
     for (int c = t * 8; c < s.d; c += s.tpr * 8) {
-      float v[8];
-      load8(q + m * ldq, c, s.d, v);
+      Raw8<int8_t, WHOLE> raw;
+      Raw8<T, WHOLE> raw_g;
+      raw.load(q + m * ldq, c, s.d);
       const float scale = code_scale(code[m * ldc + c / kPackBlock]);
+      if (kSilu && out) raw_g.load(grad + m * ldg, c, s.d);
+      float v[8];
+      raw.values(v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= scale;
       if constexpr (kSilu) {
+        Sigmoid f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = sigmoid(v[j]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= f[j].s;
         if (out) {
           float g[8];
-          load8(grad + m * ldg, c, s.d, g);
+          raw_g.values(g);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) g[j] *= silu_d1(v[j]);
-          store8(out + m * ldo, c, s.d, g);
+          for (int j = 0; j < 8; ++j) g[j] *= f[j].s + v[j] * f[j].c;
+          store8<WHOLE>(out + m * ldo, c, s.d, g);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = silu(v[j]);
       }
-      if (value) store8(value + m * ldv, c, s.d, v);
+      if (value) store8<WHOLE>(value + m * ldv, c, s.d, v);
     }
   }
 }
@@ -568,6 +595,13 @@ static unsigned pack_grid(const PackShape& s) {
   const long long need = (s.rows + 256 / s.tpr - 1) / (256 / s.tpr);
   return (unsigned)(need < 8192 ? need : 8192);
 }
+// Unpacking: workgroups that take several rows each spare a short call the set-up per row (200 000 x 200 bf16, SiLU and
+// gradient, 48 us with 8192 workgroups, 58 with as many as rows allow); in a long call they drift apart over the memory
+// (150 001 x 2048: 449 us with 8192, 396 with 32 768, 384 with 65 536).
+static unsigned unpack_grid(const PackShape& s) {
+  const long long need = (s.rows + 256 / s.tpr - 1) / (256 / s.tpr), most = need < 32768 ? 8192 : 65536;
+  return (unsigned)(need < most ? need : most);
+}
 
 static int check_packed(const void* q, int64_t ldq, const void* code, int64_t ldc, int64_t rows, int32_t d, int type) {
   if (rows < 0 || rows > INT_MAX || d < 1 || !type_known(type)) return JANUS_EINVAL;
@@ -607,13 +641,17 @@ extern "C" int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* co
   const PackShape s = pack_shape(rows, d);
   with_type(type, [&](auto zero) {
     using T = decltype(zero);
-    auto go = [&](auto silu) {
-      hipLaunchKernelGGL((unpack_rows_kernel<T, decltype(silu)::value>), dim3(pack_grid(s)), dim3(256), 0,
-                         static_cast<hipStream_t>(stream), s, q, ldq, code, ldc, static_cast<const T*>(grad), ldg,
-                         static_cast<T*>(out), ldo, static_cast<T*>(value), ldv);
+    auto go = [&](auto silu, auto whole) {
+      hipLaunchKernelGGL((unpack_rows_kernel<T, decltype(silu)::value, decltype(whole)::value>), dim3(unpack_grid(s)),
+                         dim3(256), 0, static_cast<hipStream_t>(stream), s, q, ldq, code, ldc,
+                         static_cast<const T*>(grad), ldg, static_cast<T*>(out), ldo, static_cast<T*>(value), ldv);
     };
-    if (act == JANUS_ACT_SILU) go(std::true_type{});
-    else go(std::false_type{});
+    auto by_width = [&](auto silu) {
+      if (d % 8 == 0) go(silu, std::true_type{});
+      else go(silu, std::false_type{});
+    };
+    if (act == JANUS_ACT_SILU) by_width(std::true_type{});
+    else by_width(std::false_type{});
   });
   return launched();
 }

@@ -1,0 +1,40 @@
+"""Values of the operators around an expert block where few bits or special values show."""
+import pytest
+
+from helpers import banner
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+
+
+def _dt(t):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[t]
+
+
+def test_unpacked_silu_far_from_zero():
+    """SiLU and SiLU' of stored values from -104 to 104 in fp32.  With e = exp(-|a|): the hardware exponential is good
+    to 2 E of itself on [2^-1/2, 2^1/2], where its argument is off by at most 2^-25 (0.4 E of the result), and the
+    power of two beside it is exact; 1 + e adds E to at most half of that, the reciprocal 2 E, and a product E each: 7.6 E for
+    s = 1 / (1 + e) or e / (1 + e), and for 1 - s, 8.6 E for a s.  SiLU' = s + (a s) (1 - s) takes 17.2 E of its second
+    term and E of the sum, the gradient E.  Below fp32's normal range a value is off by half a step of 2^-149, |a| times as
+    much where it is multiplied by a."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("unpack silu far")
+    n = torch.arange(-104, 105, dtype=torch.float64)
+    a = torch.cat([n, n / 8, n / 1024, 2.0 ** -torch.arange(1, 100, dtype=torch.float64)])
+    a = a[a != 0].reshape(-1, 1)                    # a row each, so each has a scale of its own and is kept exactly
+    p = janus.pack_rows(a.float().cuda())
+    assert torch.equal(janus.unpack_rows(p, torch.float32).cpu().double(), a)
+    g = torch.full_like(a, 0.75).float()
+    dx, value = janus.unpack_rows(p, torch.float32, act="silu", grad=g.cuda(), value=True)
+    e = torch.exp(-a.abs())
+    s, c = torch.where(a > 0, 1 / (1 + e), e / (1 + e)), torch.where(a > 0, e / (1 + e), 1 / (1 + e))
+    small = (a.abs() + 2) * 2.0 ** -149
+    want, dwant = a * s, g.double() * (s + a * s * c)
+    over = ((value.cpu().double() - want).abs() - (9 * E * want.abs() + small)).max().item()
+    assert over <= 0, over
+    dover = ((dx.cpu().double() - dwant).abs() - g.double() * (10 * E * s + 21 * E * (a * s * c).abs()) - small).max().item()
+    assert dover <= 0, dover
