@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * kExpertWaves) void expert_up_kernel(ExpertArgs
   for (int base = 0; base < s.count; base += 16 * MT)
     expert_product<T, T, Eight<T>, COLS, MT>(s, base, x, ldx, a.k, w1 + (long long)s.expert * a.d * a.h, a.h, 0, a.d,
                                              a.d, deep_waves(a.d), lds, [&](int t, int c, float v) {
-                                               hidden[(long long)s.slot[t] * a.h + c] = silu(v);
+                                               hidden[(long long)s.slot[t] * a.h + c] = v * sigmoid(v).s;
                                              });
   if constexpr (kRoute) {   // the gates are not needed before
     if (blockIdx.x == 0 && blockIdx.y == 0) {

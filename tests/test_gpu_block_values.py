@@ -38,3 +38,26 @@ def test_unpacked_silu_far_from_zero():
     assert over <= 0, over
     dover = ((dx.cpu().double() - dwant).abs() - g.double() * (10 * E * s + 21 * E * (a * s * c).abs()) - small).max().item()
     assert dover <= 0, dover
+
+
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_hidden_silu_far_from_zero(tokens):
+    """A hidden value of a large negative pre-activation, taken out by weights of one: 8.6 E for SiLU (see above) and
+    nothing for products with one and zero."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("expert_layer silu far", tokens)
+    x = torch.zeros(tokens, 16)
+    x[:, 0] = -20.25 - 3.1875 * torch.arange(tokens)
+    if tokens == 1:
+        x[0, 0] = -80.8125
+    up = torch.zeros(1, 16, 16)
+    up[0, 0] = 1.0 + torch.arange(16) / 1024        # a row of pre-activations, products rounded once
+    down = torch.eye(16)[None]
+    y, _, gate = janus.expert_layer(x.cuda(), torch.zeros(16, 1, device="cuda:0"), up.cuda(), down.cuda(), 1)
+    assert (gate == 1).all()
+    a = (x[:, :1] * up[0, :1]).double()             # as the kernel rounds the one product
+    e = torch.exp(a)
+    want = a * e / (1 + e)
+    over = ((y.cpu().double() - want).abs() - 9 * E * want.abs() - (a.abs() + 2) * 2.0 ** -149).max().item()
+    assert over <= 0, over
