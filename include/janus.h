@@ -593,8 +593,8 @@ int janus_residual_norm_grad(const janus_norm* p /* host */, const void* dr, int
  *   type         janus_type of x, y, w_up and w_down
  *   router       [d, n_experts] fp32;  beta [n_experts] fp32 or NULL (-inf masks an expert out)
  *   w_up         [n_experts, d, d_hidden];  w_down [n_experts, d_hidden, d]; 16-byte aligned
- * x and y need rows that start on 16 bytes.  With 16-bit weights the hidden values enter the second product as two
- * bf16 each (to 2^-16 of themselves, in fp32's range).  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
+ * x and y need rows that start on 16 bytes.  With 16-bit weights the hidden values enter the second product as three
+ * bf16 each, whose sum they are.  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
  * [tokens, top_k] fp32; expert ids are always valid and distinct.  A token whose logits are all -inf gets
  * gates of zero and y = 0 (an expert with a gate of zero is left out, whatever its weights hold); one with a
  * logit of NaN or +inf gets gates and y of NaN.  Neither reaches other tokens.

@@ -230,8 +230,8 @@ struct Panel {
   }
 };
 
-// Eight consecutive k of one token: as they are, or an fp32 value as the sum of two bf16 (hi rounded to
-// nearest, lo the rounded rest: together 2^-16 of the value), for products with 16-bit weights.
+// Eight consecutive k of one token: as they are, or an fp32 value as the sum of three bf16 of eight bits each (by
+// truncation, so the sum is exact), for products with 16-bit weights.
 template <typename T>
 struct Eight {
   typedef T vec __attribute__((ext_vector_type(8)));
@@ -240,17 +240,25 @@ struct Eight {
   __device__ __forceinline__ void clear() { v = vec{}; }
 };
 struct EightSplit {
-  bf16x8 hi, lo;
+  bf16x8 term[3];
   __device__ __forceinline__ void load(const float* p) {
     const f32x8 v = *reinterpret_cast<const f32x8*>(p);
+    unsigned w[3][4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      hi[j] = (__bf16)v[j];
-      const float h = (float)hi[j];
-      lo[j] = h - h == 0.f ? (__bf16)(v[j] - h) : (__bf16)0.f;
+    for (int i = 0; i < 4; ++i) {
+      float a = v[2 * i], b = v[2 * i + 1];
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const float ah = high_part(a), bh = high_part(b);
+        w[q][i] = pack_high(a, b);
+        a = a == ah ? 0.f : a - ah;   // not inf - inf
+        b = b == bh ? 0.f : b - bh;
+      }
     }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) term[q] = __builtin_bit_cast(bf16x8, make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]));
   }
-  __device__ __forceinline__ void clear() { hi = bf16x8{}, lo = bf16x8{}; }
+  __device__ __forceinline__ void clear() { term[0] = term[1] = term[2] = bf16x8{}; }
 };
 
 // column c of a panel of 16-bit values: eight k in order
@@ -291,8 +299,9 @@ __device__ __forceinline__ void multiply(const EightSplit& a, const Panel<__bf16
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
     const bf16x8 b = __builtin_bit_cast(bf16x8, panel_column(w, c));
-    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.lo, b, acc[c], 0, 0, 0);
-    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.hi, b, acc[c], 0, 0, 0);
+#pragma unroll
+    for (int q = 2; q >= 0; --q)   // small terms first
+      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], b, acc[c], 0, 0, 0);
   }
 }
 // An fp16 weight is exactly the sum of two bf16 (eight and three bits of it), whose range the hidden values
@@ -305,18 +314,17 @@ __device__ __forceinline__ void multiply(const EightSplit& a, const Panel<_Float
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float x = (float)w.row[2 * i][c], y = (float)w.row[2 * i + 1][c];
-      const unsigned xb = __float_as_uint(x), yb = __float_as_uint(y);
-      hi[i] = __builtin_amdgcn_perm(yb, xb, 0x07060302u);
-      const float xh = __uint_as_float(xb & 0xFFFF0000u), yh = __uint_as_float(yb & 0xFFFF0000u);
-      const float xl = x == xh ? 0.f : x - xh, yl = y == yh ? 0.f : y - yh;   // not inf - inf
-      lo[i] = __builtin_amdgcn_perm(__float_as_uint(yl), __float_as_uint(xl), 0x07060302u);
+      const float xh = high_part(x), yh = high_part(y);
+      hi[i] = pack_high(x, y);
+      lo[i] = pack_high(x == xh ? 0.f : x - xh, y == yh ? 0.f : y - yh);   // not inf - inf
     }
     const bf16x8 bh = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
     const bf16x8 bl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.lo, bl, acc[c], 0, 0, 0);
-    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.lo, bh, acc[c], 0, 0, 0);
-    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.hi, bl, acc[c], 0, 0, 0);
-    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.hi, bh, acc[c], 0, 0, 0);
+#pragma unroll
+    for (int q = 2; q >= 0; --q) {   // small terms first
+      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], bl, acc[c], 0, 0, 0);
+      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], bh, acc[c], 0, 0, 0);
+    }
   }
 }
 

@@ -191,11 +191,6 @@ struct Terms<float> {
   static constexpr int kPlanes = 3, kCols = 128;
 };
 
-__device__ __forceinline__ unsigned pack_high(float a, float b) {   // the upper halves, a first
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-}
-__device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
-
 // Where the rows of both operands start on four bytes (WORDS: always for fp32), a chunk's rows are a buffer: words
 // behind the one that holds its last value are zero, so its ragged end needs no code.  Past a row's end a run goes on
 // into the next one; those columns are not stored.  Other rows are read by runs at any address in the same way, but

@@ -71,6 +71,12 @@ __device__ __forceinline__ Sigmoid sigmoid(float a) {
   return a < 0.f ? Sigmoid{small, large} : Sigmoid{large, small};
 }
 
+// An fp32 value's first eight bits, which bf16 holds, and two values' as a pair, a first.
+__device__ __forceinline__ float high_part(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
+__device__ __forceinline__ unsigned pack_high(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+
 inline bool type_known(int t) { return t == JANUS_F32 || t == JANUS_BF16 || t == JANUS_F16; }
 inline int type_bytes(int t) { return t == JANUS_F32 ? 4 : 2; }
 

@@ -61,3 +61,34 @@ def test_hidden_silu_far_from_zero(tokens):
     want = a * e / (1 + e)
     over = ((y.cpu().double() - want).abs() - 9 * E * want.abs() - (a.abs() + 2) * 2.0 ** -149).max().item()
     assert over <= 0, over
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens", [1, 5, 64])
+def test_hidden_values_keep_their_bits(tokens, t):
+    """Two hidden values near 1, 2^-15 apart, whose difference the second product forms with weights of 1 and -1.
+    Pre-activations are exact; a hidden value is off by 8.6 E of itself, its products are exact, and at most six
+    additions (three terms of each, zeros add nothing) cut off up to 2 E of the values' sum."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("expert_layer hidden bits", tokens, t)
+    dt = _dt(t)
+    x = torch.zeros(tokens, 16)
+    x[:, 0] = 1.3125 + torch.arange(tokens) / 64
+    x[:, 1] = 2.0 ** -8
+    up = torch.zeros(1, 16, 16)
+    up[0, 0, :2] = 1.0
+    up[0, 1, 1] = 2.0 ** -7
+    down = torch.zeros(1, 16, 16)
+    down[0, 0, :] = -1.0
+    down[0, 1, :] = 1.0
+    x, up, down = x.to(dt), up.to(dt), down.to(dt)
+    y, _, gate = janus.expert_layer(x.cuda(), torch.zeros(16, 1, device="cuda:0"), up.cuda(), down.cuda(), 1)
+    assert (gate == 1).all()
+    h = torch.nn.functional.silu(x.double() @ up[0].double())[:, :2]
+    want = (h[:, 1] - h[:, 0])[:, None]
+    size = h.sum(1, keepdim=True)
+    u = torch.finfo(dt).eps / 2
+    tiny = 2.0 ** -25 if t == "f16" else 0.0
+    over = ((y.cpu().double() - want).abs() - (u * want.abs() + (9 + 12) * E * size * (1 + u) + tiny)).max().item()
+    assert over <= 0, over
