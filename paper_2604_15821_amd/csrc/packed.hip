@@ -202,6 +202,15 @@ __device__ __forceinline__ buffer rows_buffer(const void* p, unsigned bytes) {
 }
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// What plane q leaves of a value.  Not inf - inf: an infinity leaves zero, in fp16, whose second plane is the last, itself (by
+// one instruction in place of two: 2.5 % of the call against 5; fp32, 3 %).
+template <typename T>
+__device__ __forceinline__ float rest(float a, int q) {
+  const float high = high_part(a);
+  if constexpr (std::is_same_v<T, _Float16>) return a - __builtin_amdgcn_fmed3f(high, -65504.0f, 65504.0f);
+  return q == 0 && a == high ? 0.f : a - high;
+}
+
 // Eight values of a row of B, and their planes.
 template <typename T>
 struct Octet {
@@ -239,8 +248,8 @@ struct Octet {
 #pragma unroll
         for (int q = 0; q < Terms<T>::kPlanes; ++q) {
           w[q][i] = pack_high(a, b);
-          a -= high_part(a);
-          b -= high_part(b);
+          a = rest<T>(a, q);
+          b = rest<T>(b, q);
         }
       }
 #pragma unroll

@@ -92,3 +92,25 @@ def test_hidden_values_keep_their_bits(tokens, t):
     tiny = 2.0 ** -25 if t == "f16" else 0.0
     over = ((y.cpu().double() - want).abs() - (u * want.abs() + (9 + 12) * E * size * (1 + u) + tiny)).max().item()
     assert over <= 0, over
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_infinity_in_a_gradient_stays_one(t):
+    """G = X^T B with an infinity in B: an infinity of X's sign in its column, NaN where X is zero."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("packed_wgrad infinity", t)
+    x = torch.randn(90, 40, generator=torch.Generator().manual_seed(1))
+    x[30, 7] = x[60, 9] = 0.0
+    b = torch.randn(90, 24, generator=torch.Generator().manual_seed(2)).to(_dt(t))
+    b[30, 3] = float("inf")
+    b[60, 11] = -float("inf")
+    b[75, 20] = float("nan")
+    p = janus.pack_rows(x.cuda())
+    X = janus.unpack_rows(p, torch.float32).cpu().double()
+    off = torch.tensor([0, 70, 90], dtype=torch.int32)
+    got = janus.packed_wgrad(p, b.cuda(), off.cuda()).cpu()
+    want = torch.stack([X[m0:m1].t().contiguous() @ b[m0:m1].double() for m0, m1 in ((0, 70), (70, 90))])
+    assert torch.isposinf(want).any() and torch.isneginf(want).any() and torch.isnan(want).any()
+    for kind in (torch.isposinf, torch.isneginf, torch.isnan):
+        assert torch.equal(kind(got), kind(want))
