@@ -114,6 +114,19 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackShape s, const T* __
   }
 }
 
+// The largest finite values of a type are rounded up to 64 steps of the largest code that they get, which is beyond the
+// type: such a value reads as the largest finite one, which is nearer to them than the half step that rounding may cost.
+template <typename T>
+struct Top {
+  static constexpr int kCode = 249;
+  static constexpr float kOver = INFINITY, kMost = std::is_same_v<T, float> ? 0x1.fffffep127f : 0x1.fep127f;
+};
+template <>
+struct Top<_Float16> {
+  static constexpr int kCode = 137;
+  static constexpr float kOver = 65536.0f, kMost = 65504.0f;
+};
+
 // value = x, or SiLU(x) and out = grad SiLU'(x), of the stored x.  Widths that are multiples of eight have no code for a
 // row's end, so that all loads of a thread are in flight together.
 template <typename T, bool kSilu, bool WHOLE>
@@ -127,12 +140,18 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
       Raw8<int8_t, WHOLE> raw;
       Raw8<T, WHOLE> raw_g;
       raw.load(q + m * ldq, c, s.d);
-      const float scale = code_scale(code[m * ldc + c / kPackBlock]);
+      const int power = code[m * ldc + c / kPackBlock];
       if (kSilu && out) raw_g.load(grad + m * ldg, c, s.d);
       float v[8];
       raw.values(v);
+      const float scale = code_scale(power);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= scale;
+      if (power == Top<T>::kCode) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (fabsf(v[j]) == Top<T>::kOver) v[j] = copysignf(Top<T>::kMost, v[j]);
+      }
       if constexpr (kSilu) {
         Sigmoid f[8];
 #pragma unroll

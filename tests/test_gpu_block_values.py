@@ -114,3 +114,37 @@ def test_infinity_in_a_gradient_stays_one(t):
     assert torch.isposinf(want).any() and torch.isneginf(want).any() and torch.isnan(want).any()
     for kind in (torch.isposinf, torch.isneginf, torch.isnan):
         assert torch.equal(kind(got), kind(want))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_finite_activations_come_back_finite(t):
+    """A block's rounding can carry the largest values of a type one step beyond it; they come back as its largest
+    finite value, and every value within max(max|x| / 127, 2^-127) of its block."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("pack_rows top", t)
+    dt = _dt(t)
+    top = torch.finfo(dt).max
+    x = torch.linspace(-1, 1, 96, dtype=torch.float64).repeat(6, 1)
+    for m, s in enumerate((1.0, 1 - 2.0 ** -7, 1 - 2.0 ** -6, 0.5, 2.0 ** -8)):
+        x[m] *= top * s
+    x[5] = top
+    x[5, 40] = -top
+    x = x.to(dt)
+    p = janus.pack_rows(x.cuda())
+    size = x.double().abs().view(6, 3, 32).amax(2).repeat_interleave(32, 1)
+    for act in ("none", "silu"):
+        got = janus.unpack_rows(p, dt, act=act).cpu()
+        assert torch.isfinite(got).all()
+        if act == "none":
+            assert ((got.double() - x.double()).abs() <= (size / 127).clamp(min=2.0 ** -127)).all()
+            assert (got[5, :40] == top).all() and got[5, 40] == -top
+    g = torch.ones(6, 96, dtype=dt)
+    dx, value = janus.unpack_rows(p, dt, act="silu", grad=g.cuda(), value=True)
+    assert torch.isfinite(dx).all() and torch.isfinite(value).all()
+    x[2, 5] = float("inf")
+    got = janus.unpack_rows(janus.pack_rows(x.cuda()), dt).cpu()
+    assert torch.isnan(got[2, :32]).all() and torch.isfinite(got[2, 32:]).all()
+    wide = torch.tensor([[1e6], [-1e6]], device="cuda:0")      # beyond fp16: as a conversion would have it
+    assert torch.equal(janus.unpack_rows(janus.pack_rows(wide), torch.float16).cpu(),
+                       torch.tensor([[float("inf")], [-float("inf")]], dtype=torch.float16))
