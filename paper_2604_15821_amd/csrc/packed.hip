@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "chunk_cut.h"
 #include "rows.h"
 
 namespace janus {
@@ -505,9 +506,8 @@ __global__ __launch_bounds__(1024) void packed_chunks_kernel(const int* __restri
     a = min(max(off[g], 0), (int)rows);
     size = max(min(max(off[g + 1], 0), (int)rows) - a, 0);
   }
-  const int mine = (size + kc - 1) / kc;
-  const int each = mine ? ((size + mine - 1) / mine + kWgRows - 1) / kWgRows * kWgRows : 0;
-  const int n = g >= groups ? 0 : mine ? (size + each - 1) / each : 1;   // a group without rows: one empty chunk
+  const ChunkCut cut = chunk_cut(size, kc, kWgRows);
+  const int each = cut.each, n = g < groups ? cut.count : 0;
   size_n[g] = make_int2(each, n);
   __syncthreads();
   int at = 0, all = 0;

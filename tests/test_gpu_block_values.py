@@ -148,3 +148,22 @@ def test_finite_activations_come_back_finite(t):
     wide = torch.tensor([[1e6], [-1e6]], device="cuda:0")      # beyond fp16: as a conversion would have it
     assert torch.equal(janus.unpack_rows(janus.pack_rows(wide), torch.float16).cpu(),
                        torch.tensor([[float("inf")], [-float("inf")]], dtype=torch.float16))
+
+
+def test_weight_gradient_of_the_most_rows():
+    """2^31 - 4097 rows of one column, in one group and in two: every row is in one chunk, and the few that are not
+    zero add up exactly."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("packed_wgrad most rows")
+    rows = 2 ** 31 - 4097
+    p = janus.PackedRows(torch.full((rows, 1), 64, dtype=torch.int8, device="cuda:0"),
+                         torch.full((rows, 1), 121, dtype=torch.uint8, device="cuda:0"))   # ones
+    B = torch.zeros(rows, 1, dtype=torch.bfloat16, device="cuda:0")
+    at = [0, 1, 16_223, 16_224, 2 ** 30, 2 ** 30 + 12_345, rows - 16_225, rows - 6, rows - 5, rows - 1]
+    for k, m in enumerate(at):
+        B[m] = 2.0 ** k
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda:0")
+    assert janus.packed_wgrad(p, B, off).item() == 1023
+    off = torch.tensor([0, rows - 5, rows], dtype=torch.int32, device="cuda:0")
+    assert janus.packed_wgrad(p, B, off).view(-1).tolist() == [255, 768]
