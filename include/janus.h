@@ -626,7 +626,8 @@ int janus_expert_layer(const janus_experts* p /* host */, const void* x, int64_t
  * it (2^128, fp16: 2^16); janus_unpack_rows gives the type's largest finite value for that, janus_packed_wgrad takes 2^128 as
  * an infinity.  A block with an infinity or NaN gets c = 255 and q = 0 and reads as NaN; c = 0, which no block
  * gets, reads as zeros.
- *   q [rows, d] int8, rows ldq apart;  code [rows, ceil(d / 32)] uint8, rows ldc apart.
+ *   q [rows, d] int8, rows ldq apart;  code [rows, ceil(d / 32)] uint8, rows ldc apart; rows below 2^31, d
+ *   at most 2^31 - 4097 (wider: JANUS_EUNSUPPORTED).
  * Columns of q between d and ldq, and of code behind the last block, are neither read into a result nor written.
  */
 int janus_pack_rows(const void* x, int64_t ldx, int32_t type, int64_t rows, int32_t d, int8_t* q, int64_t ldq,

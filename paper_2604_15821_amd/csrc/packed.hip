@@ -626,8 +626,11 @@ static unsigned unpack_grid(const PackShape& s) {
   return (unsigned)(need < most ? need : most);
 }
 
+// Columns are counted in 32 bits, a step of the widest rows' threads (2048) behind the last one included.
+constexpr int kWidest = INT_MAX - 4096;
 static int check_packed(const void* q, int64_t ldq, const void* code, int64_t ldc, int64_t rows, int32_t d, int type) {
   if (rows < 0 || rows > INT_MAX || d < 1 || !type_known(type)) return JANUS_EINVAL;
+  if (d > kWidest) return JANUS_EUNSUPPORTED;
   if (rows > 0 && (!q || !code || ldq < d || ldc < (d + kPackBlock - 1) / kPackBlock)) return JANUS_EINVAL;
   return JANUS_OK;
 }

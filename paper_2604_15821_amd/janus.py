@@ -529,6 +529,8 @@ ACT = {"none": 0, "silu": 1}
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
+_MOST = 2 ** 31 - 1   # of what the library counts in 32 bits: ctypes would cut off more without a word
+
 
 def _type_of(t, name):
     """janus_type of a tensor or of a torch dtype."""
@@ -577,7 +579,16 @@ def _matrix(t, name):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if t.dim() != 2:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected two dimensions")
+    if t.shape[1] > _MOST:
+        raise ValueError(f"{name}: {t.shape[1]} columns, at most {_MOST}")
     return t.shape[0], t.shape[1], t.device
+
+
+def _offsets(t, name, device):
+    """Check the offsets of groups or sequences; returns how many of these there are."""
+    if isinstance(t, torch.Tensor) and t.numel() > _MOST:
+        raise ValueError(f"{name}: {t.numel()} offsets, at most {_MOST}")
+    return _arg(t, name, "i32", (None,), device).shape[0] - 1
 
 
 def _call(rc, where):
@@ -605,8 +616,7 @@ def _norm(rows, d, like, device, w_post, gate, gate_off, scale, w_pre, eps):
     if gate_off is not None:
         if gate is None:
             raise ValueError("gate_off: without a gate")
-        _arg(gate_off, "gate_off", "i32", (None,), device)
-        p.n_seq = gate_off.shape[0] - 1
+        p.n_seq = _offsets(gate_off, "gate_off", device)
         if p.n_seq < 0:
             raise ValueError("gate_off: needs at least one offset")
         p.gate_off = gate_off.data_ptr()
@@ -714,12 +724,17 @@ def expert_layer(x, router, w_up, w_down, top_k, beta=None, normalize=False, out
     if not isinstance(w_up, torch.Tensor) or w_up.dim() != 3:
         raise ValueError("w_up: expected a tensor [experts, d, hidden]")
     n, _, h = w_up.shape
+    if n > _MOST or h > _MOST:
+        raise ValueError(f"w_up: {n} experts of {h} hidden values, at most {_MOST} of both")
+    top_k = int(top_k)
+    if not -_MOST <= top_k <= _MOST:
+        raise ValueError(f"top_k: {top_k}, at most {_MOST}")
     code = _type_of(x, "x")
     px, ldx = _rows(x, "x", x.dtype, (tokens, d), dev)
     pr = _weights(router, "router", torch.float32, (d, n), dev)
     pu = _weights(w_up, "w_up", x.dtype, (n, d, h), dev)
     pw = _weights(w_down, "w_down", x.dtype, (n, h, d), dev)
-    p = Experts(d, h, n, int(top_k), code, int(bool(normalize)), pr, _param(beta, "beta", n, dev), pu, pw)
+    p = Experts(d, h, n, top_k, code, int(bool(normalize)), pr, _param(beta, "beta", n, dev), pu, pw)
     lib = _lib()
     size = _call(lib.janus_expert_layer_workspace(C.byref(p), tokens), "janus_expert_layer_workspace")
     y = torch.empty(tokens, d, dtype=x.dtype, device=dev) if out is None else out
@@ -798,8 +813,7 @@ def packed_wgrad(packed, B, row_off, out=None):
     n, Q, _ = _matrix(B, "B")
     code = _type_of(B, "B")
     pb, ldb = _rows(B, "B", B.dtype, (rows, Q), dev)
-    _arg(row_off, "row_off", "i32", (None,), dev)
-    G = row_off.shape[0] - 1
+    G = _offsets(row_off, "row_off", dev)
     if out is None:
         out = torch.empty(max(G, 0), P, Q, dtype=torch.float32, device=dev)
     else:

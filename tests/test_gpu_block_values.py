@@ -167,3 +167,17 @@ def test_weight_gradient_of_the_most_rows():
     assert janus.packed_wgrad(p, B, off).item() == 1023
     off = torch.tensor([0, rows - 5, rows], dtype=torch.int32, device="cuda:0")
     assert janus.packed_wgrad(p, B, off).view(-1).tolist() == [255, 768]
+
+
+def test_the_widest_row():
+    """One row of 2^31 - 4097 columns through packing and unpacking."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("pack_rows widest")
+    d = 2 ** 31 - 4097
+    x = torch.zeros(1, d, dtype=torch.bfloat16, device="cuda:0")
+    for k, c in enumerate((0, 2047, 2 ** 30 + 5, d - 2049, d - 9, d - 1)):
+        x[0, c] = 1.0 + k
+    p = janus.pack_rows(x)
+    assert p.code.shape == (1, 2 ** 26 - 128) and p.q[0, -1] == 96 and p.code[0, -1] == 123   # 6 = 96 / 16
+    assert torch.equal(janus.unpack_rows(p, torch.bfloat16), x)
