@@ -650,8 +650,8 @@ int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t
  * result).  1..1024 groups, rows at most 2^31 - 4097; groups without rows get zeros.  Every product is exact in fp32;
  * sums are held in fp32 and split over row chunks that are added in a fixed order.  An infinity or NaN of B reaches its own column,
  * a block of X that holds one its own rows.  Offsets that break these rules give wrong values but no access outside
- * the arrays.  Rows of q and B that start on multiples of four bytes are read fastest; rows of more than 256 KB may be
- * refused (JANUS_EUNSUPPORTED), and sizes that one launch cannot hold are, by both functions.
+ * the arrays.  Rows of q and B that start on multiples of four bytes are read fastest; rows more than 262 144 bytes
+ * apart may be refused (JANUS_EUNSUPPORTED), and sizes that one launch cannot hold are, by both functions.
  */
 int64_t janus_packed_wgrad_workspace(int64_t rows, int32_t n_groups, int32_t P, int32_t Q, int32_t type);
 int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t ldc, const void* B, int64_t ldb,

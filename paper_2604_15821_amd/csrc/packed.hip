@@ -586,9 +586,10 @@ struct WgradPlan {
 // last chunks are ragged), chunks that fill them in one round; else half of what each would get of all rows, so
 // that the last ones end together.  (One group of 65 536 rows, 512 x 2048, bf16: 227 us by the second rule, 185 by the first.)
 // Not below 512 rows, where partials cost more than they save (100 000 rows, 4 groups, 128 x 128, bf16: 29 us at 512,
-// 36 at 256), nor above 16 384, so that a chunk's bytes stay within the 32-bit offsets of a buffer for rows of up to
-// 256 KB.
-constexpr int kMostChunkRows = 16384, kWgSlots = 512;
+// 36 at 256), nor above 16 224, so that the bytes of a chunk and of the 128 rows that reads may run ahead stay within the
+// 32-bit offsets of a buffer for rows of up to 256 KB.
+constexpr int kMostChunkRows = 16224, kReadAhead = 4 * kWgRows, kWgSlots = 512;
+static_assert((kMostChunkRows + kReadAhead) * 262144ll <= UINT_MAX && kMostChunkRows % kWgRows == 0);
 static WgradPlan wgrad_plan(int64_t rows, int groups, int P, int Q, int type) {
   WgradPlan w;
   w.tiles_p = (int)cdiv(P, kWgP);
@@ -702,13 +703,13 @@ extern "C" int janus_packed_wgrad(const int8_t* q, int64_t ldq, const uint8_t* c
   int rc = check_packed_wgrad(rows, n_groups, P, Q, type);
   if (!rc) rc = check_packed(q, ldq, code, ldc, rows, P, type);
   if (rc) return rc;
+  const WgradPlan w = wgrad_plan(rows, n_groups, P, Q, type);
+  if (rows > 0 && (ldb > UINT_MAX || std::max({ldq, ldc, ldb * type_bytes(type)}) > UINT_MAX / (w.kc + kReadAhead)))
+    return JANUS_EUNSUPPORTED;
   if (!G || !row_off || (rows > 0 && (!B || ldb < Q)) || !work || !rows_aligned(work, 0, 1) ||
       work_bytes < janus_packed_wgrad_workspace(rows, n_groups, P, Q, type))
     return JANUS_EINVAL;
-  const WgradPlan w = wgrad_plan(rows, n_groups, P, Q, type);
   const int64_t blocks = (int64_t)wgrad_blocks(w);
-  const int64_t row_bytes = std::max({ldq, ldc, ldb * type_bytes(type)});
-  if (rows > 0 && row_bytes > (int64_t)UINT_MAX / (w.kc + 4 * kWgRows)) return JANUS_EUNSUPPORTED;
   char* base = static_cast<char*>(work);
   int* n_chunks = reinterpret_cast<int*>(base);
   PackedChunk* chunks = reinterpret_cast<PackedChunk*>(base + w.chunks);

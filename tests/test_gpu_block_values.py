@@ -181,3 +181,21 @@ def test_the_widest_row():
     p = janus.pack_rows(x)
     assert p.code.shape == (1, 2 ** 26 - 128) and p.q[0, -1] == 96 and p.code[0, -1] == 123   # 6 = 96 / 16
     assert torch.equal(janus.unpack_rows(p, torch.bfloat16), x)
+
+
+def test_weight_gradient_of_rows_256_kib_apart():
+    """Chunks of 16 224 rows, 262 144 bytes apart: offsets up to the end of 32 bits, the same values as rows side by side."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("packed_wgrad far rows")
+    rows, P, Q, ld = 33_000, 2048, 4096, 1 << 18
+    g = torch.Generator(device="cuda:0").manual_seed(6)
+    p = janus.pack_rows(torch.randn(rows, P, generator=g, device="cuda:0"))
+    B = torch.randn(rows, Q, generator=g, device="cuda:0").bfloat16()
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda:0")
+    q = torch.empty(rows * ld, dtype=torch.int8, device="cuda:0").as_strided((rows, P), (ld, 1))
+    q.copy_(p.q)
+    assert torch.equal(janus.packed_wgrad(janus.PackedRows(q, p.code), B, off), janus.packed_wgrad(p, B, off))
+    far = torch.empty(rows * ld // 2, dtype=torch.bfloat16, device="cuda:0").as_strided((rows, Q), (ld // 2, 1))
+    far.copy_(B)
+    assert torch.equal(janus.packed_wgrad(p, far, off), janus.packed_wgrad(p, B, off))

@@ -42,3 +42,21 @@ def test_binding_counts():
     for name in ("row_off", "gate_off"):
         with pytest.raises(ValueError, match=f"{name}: .* at most"):
             janus._offsets(_meta(wide, dtype=torch.int32), name, y.device)
+
+
+@pytest.mark.parametrize("rows", [1, 10_000, 1 << 24, 2 ** 31 - 4097])
+def test_distances_of_rows_up_to_256_kib(rows):
+    """The packed weight gradient takes rows 262 144 bytes apart at any number of rows (the call then asks for its
+    scratch memory, which is not given), and no more than its 32-bit offsets reach at the longest chunks."""
+    lib = janus._lib()
+
+    def call(ldq, ldc, ldb, t):
+        return lib.janus_packed_wgrad(P, ldq, P, ldc, P, ldb, t, P, P, 1, rows, 40, 24, None, 0, None)
+    far = 1 << 18
+    for t, size in ((0, 4), (1, 2), (2, 2)):
+        for ld in ((far, 2, 24), (40, far, 24), (40, 2, far // size), (far, far, far // size)):
+            assert call(*ld, t) == janus.JANUS_EINVAL, ld
+        for ld in ((1 << 23, 2, 24), (40, 1 << 23, 24), (40, 2, (1 << 23) // size), (40, 2, (1 << 62) + 24)):
+            assert call(*ld, t) == EUNSUP, ld
+        if rows >= 1 << 24:
+            assert call(263_000, 2, 24, t) == EUNSUP
