@@ -622,7 +622,7 @@ int janus_expert_layer(const janus_experts* p /* host */, const void* x, int64_t
  * Activations in 8 bits.  The columns of a row are cut into blocks of 32; a block holds int8
  * values q and one code byte c and stands for q 2^(c - 127).  The power of two is the least with
  * max|x| <= 127 2^(c - 127), but not below 2^-126; values are rounded to nearest, ties to even, so
- * each is off by at most max|x| / 127 of its block.  The largest values of a type may round to a power of two beyond
+ * each is off by at most max|x| / 127 of its block or 2^-127, whichever is more.  The largest values of a type may round to a power of two beyond
  * it (2^128, fp16: 2^16); janus_unpack_rows gives the type's largest finite value for that, janus_packed_wgrad takes 2^128 as
  * an infinity.  A block with an infinity or NaN gets c = 255 and q = 0 and reads as NaN; c = 0, which no block
  * gets, reads as zeros.

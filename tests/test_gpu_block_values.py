@@ -199,3 +199,26 @@ def test_weight_gradient_of_rows_256_kib_apart():
     far = torch.empty(rows * ld // 2, dtype=torch.bfloat16, device="cuda:0").as_strided((rows, Q), (ld // 2, 1))
     far.copy_(B)
     assert torch.equal(janus.packed_wgrad(p, far, off), janus.packed_wgrad(p, B, off))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_rounding_of_every_block(t):
+    """Half a step: at most max|x| / 127 of the block, and 2^-127 where the step is 2^-126 (blocks below 127 2^-126)."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("pack_rows bound", t)
+    dt = _dt(t)
+    low = -149 if t == "f32" else -133 if t == "bf16" else -24
+    e = torch.arange(low, 13 if t == "f16" else 125, dtype=torch.float64)
+    g = torch.Generator().manual_seed(8)
+    x = (torch.rand(len(e), 64, generator=g, dtype=torch.float64) * 2 - 1) * 2.0 ** e[:, None]
+    x[:, ::5] = x[:, ::5].sign() * 2.0 ** e[:, None]
+    x = x.to(dt)
+    p = janus.pack_rows(x.cuda())
+    step = (p.code.cpu().double() - 127).exp2().repeat_interleave(32, 1)
+    got = p.q.cpu().double() * step
+    size = x.double().abs().view(-1, 2, 32).amax(2).repeat_interleave(32, 1)
+    assert ((got - x.double()).abs() <= (size / 127).clamp(min=2.0 ** -127)).all()
+    if t == "f32":
+        assert (got[0] == 0).all() and (size[0] == 2.0 ** -149).all()      # below half of the least step
+        assert torch.equal(janus.unpack_rows(p, torch.float32).cpu().double(), got)
