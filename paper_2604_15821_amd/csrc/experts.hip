@@ -275,38 +275,53 @@ __device__ __forceinline__ uint4 panel_column(const Panel<T, COLS>& p, int c) {
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-template <int COLS>
+template <bool EXACT, int COLS>
 __device__ __forceinline__ void multiply(const Eight<float>& a, const Panel<float, COLS>& w, f32x4 (&acc)[COLS]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int c = 0; c < COLS; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], w.row[j][c], acc[c], 0, 0, 0);
 }
-template <int COLS>
+template <bool EXACT, int COLS>
 __device__ __forceinline__ void multiply(const Eight<__bf16>& a, const Panel<__bf16, COLS>& w, f32x4 (&acc)[COLS]) {
 #pragma unroll
   for (int c = 0; c < COLS; ++c)
     acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, __builtin_bit_cast(bf16x8, panel_column(w, c)), acc[c], 0, 0, 0);
 }
-template <int COLS>
+template <bool EXACT, int COLS>
 __device__ __forceinline__ void multiply(const Eight<_Float16>& a, const Panel<_Float16, COLS>& w, f32x4 (&acc)[COLS]) {
 #pragma unroll
   for (int c = 0; c < COLS; ++c)
     acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, __builtin_bit_cast(f16x8, panel_column(w, c)), acc[c], 0, 0, 0);
 }
-template <int COLS>
+// The smaller terms of a sum meet an infinity of the other operand as well, and zero times infinity is NaN.  Where a
+// product holds a NaN it is formed again (EXACT): they take that operand with its infinities and NaN as zeros, the largest
+// term has them.  (All terms of a value have its sign, so nothing else can go wrong.  Looking at every operand on the way
+// costs 8 % of a call.)  Two bf16 of a word: the sign bits of those that are not finite, and the word without them.
+__device__ __forceinline__ unsigned beyond(unsigned u) { return ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ unsigned finite_only(unsigned u) {
+  const unsigned m = beyond(u);
+  return u & ~(m | (m - (m >> 15)));
+}
+__device__ __forceinline__ uint4 finite_only(uint4 u) {
+  return make_uint4(finite_only(u.x), finite_only(u.y), finite_only(u.z), finite_only(u.w));
+}
+
+template <bool EXACT, int COLS>
 __device__ __forceinline__ void multiply(const EightSplit& a, const Panel<__bf16, COLS>& w, f32x4 (&acc)[COLS]) {
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
-    const bf16x8 b = __builtin_bit_cast(bf16x8, panel_column(w, c));
+    const uint4 b = panel_column(w, c);
+    uint4 f = b;
+    if (EXACT) f = finite_only(b);
 #pragma unroll
     for (int q = 2; q >= 0; --q)   // small terms first
-      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], b, acc[c], 0, 0, 0);
+      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], __builtin_bit_cast(bf16x8, q ? f : b), acc[c], 0, 0, 0);
   }
 }
 // An fp16 weight is exactly the sum of two bf16 (eight and three bits of it), whose range the hidden values
 // fit, while fp16 would cut them off at 65504 and 2^-24.
-template <int COLS>
+template <bool EXACT, int COLS>
 __device__ __forceinline__ void multiply(const EightSplit& a, const Panel<_Float16, COLS>& w, f32x4 (&acc)[COLS]) {
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
@@ -318,12 +333,15 @@ __device__ __forceinline__ void multiply(const EightSplit& a, const Panel<_Float
       hi[i] = pack_high(x, y);
       lo[i] = pack_high(x == xh ? 0.f : x - xh, y == yh ? 0.f : y - yh);   // not inf - inf
     }
-    const bf16x8 bh = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    const uint4 h = make_uint4(hi[0], hi[1], hi[2], hi[3]), top = __builtin_bit_cast(uint4, a.term[0]);
     const bf16x8 bl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+    uint4 f = h, t = top;
+    if (EXACT) f = finite_only(h), t = finite_only(top);
 #pragma unroll
     for (int q = 2; q >= 0; --q) {   // small terms first
-      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], bl, acc[c], 0, 0, 0);
-      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], bh, acc[c], 0, 0, 0);
+      const bf16x8 low = q ? a.term[q] : __builtin_bit_cast(bf16x8, t);
+      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(low, bl, acc[c], 0, 0, 0);
+      acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.term[q], __builtin_bit_cast(bf16x8, q ? f : h), acc[c], 0, 0, 0);
     }
   }
 }
@@ -381,11 +399,7 @@ __device__ __forceinline__ void expert_product(const ExpertSlots& s, int base, c
 #pragma unroll
     for (int c = 0; c < COLS; ++c) acc[m][c] = f32x4{};
   Panel<T, COLS> now, next;
-  int k = k0 + 32 * level;
-  if (k < k1) now.load(wl, n, k + sub, K);
-  for (; k < k1; k += 32 * deep) {
-    const bool more = k + 32 * deep < k1;
-    if (more) next.load(wl, n, k + 32 * deep + sub, K);
+  auto product = [&](auto exact, int k) {
     const bool behind = k + sub >= k1;
     if (behind) now.clear();
 #pragma unroll
@@ -394,9 +408,35 @@ __device__ __forceinline__ void expert_product(const ExpertSlots& s, int base, c
         A v;
         v.load(xr[m] + min(k + sub, K - 8));
         if (behind) v.clear();
-        multiply<COLS>(v, now, acc[m]);
+        multiply<exact.value, COLS>(v, now, acc[m]);
       }
+  };
+  const int first_k = k0 + 32 * level;
+  if (first_k < k1) now.load(wl, n, first_k + sub, K);
+  for (int k = first_k; k < k1; k += 32 * deep) {
+    const bool more = k + 32 * deep < k1;
+    if (more) next.load(wl, n, k + 32 * deep + sub, K);
+    product(std::false_type{}, k);
     if (more) now = next;
+  }
+  if constexpr (std::is_same_v<A, EightSplit>) {
+    bool nan = false;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int c = 0; c < COLS; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) nan |= acc[m][c][i] != acc[m][c][i];
+    if (__any(nan)) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) acc[m][c] = f32x4{};
+      for (int k = first_k; k < k1; k += 32 * deep) {
+        now.load(wl, n, k + sub, K);
+        product(std::true_type{}, k);
+      }
+    }
   }
   // row 4 (lane / 16) + i of the result, column COLS (lane % 16) + c
   for (int m = 0; m < tiles; ++m) {

@@ -222,3 +222,34 @@ def test_rounding_of_every_block(t):
     if t == "f32":
         assert (got[0] == 0).all() and (size[0] == 2.0 ** -149).all()      # below half of the least step
         assert torch.equal(janus.unpack_rows(p, torch.float32).cpu().double(), got)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_infinite_weights_give_what_the_formula_gives(tokens, t):
+    """An infinity in W_down gives an infinity of the hidden value's sign in its column, NaN where that is
+    zero; one in W_up an infinite hidden value, or NaN where x is zero or its sign the other (-inf times sigmoid(-inf))."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("expert_layer infinite weights", tokens, t)
+    g = torch.Generator().manual_seed(tokens)
+    R = lambda *s: torch.randn(*s, generator=g).to(_dt(t))  # noqa: E731
+    c = lambda v: v.cuda()  # noqa: E731
+    x, up, down = R(tokens, 32), R(1, 32, 64) / 4, R(1, 64, 48)[:, :, :32].contiguous() / 4
+    router = torch.zeros(32, 1)
+
+    def check(up, down):
+        y = janus.expert_layer(c(x), c(router), c(up), c(down), 1)[0].cpu()
+        a = x.double() @ up[0].double()
+        want = (a * torch.sigmoid(a)) @ down[0].double()
+        for kind in (torch.isposinf, torch.isneginf, torch.isnan):
+            assert torch.equal(kind(y), kind(want))
+        return want
+
+    bad = down.clone()
+    bad[0, 17, 5], bad[0, 40, 9], bad[0, 3, 30] = float("inf"), -float("inf"), float("nan")
+    want = check(up, bad)
+    assert torch.isinf(want[:, 5]).all() and torch.isinf(want[:, 9]).all() and torch.isnan(want[:, 30]).all()
+    bad = up.clone()
+    bad[0, 4, 21] = float("inf")
+    check(bad, down)
