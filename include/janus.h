@@ -525,8 +525,8 @@ int32_t janus_wgrad_chunk_rows(int64_t M, int32_t P, int32_t Q);
  * input and output are held in fp32, and outputs are rounded once (to nearest, ties to even).
  * Every address is a multiple of its element's size.  Rows that start on multiples of 16 bytes and
  * widths that are multiples of 16 bytes are read and written fastest; other layouts give the same
- * values.  Squares are summed in fp32: magnitudes stay below 1e18.  No kernel uses atomics on floating-point
- * values; results are the same on every run.
+ * values.  Squares are summed in fp32: magnitudes stay below 1e18.  No kernel adds floating-point values by
+ * atomics; results are the same on every run.
  */
 typedef enum janus_type { JANUS_F32 = 0, JANUS_BF16 = 1, JANUS_F16 = 2 } janus_type;
 typedef enum janus_act { JANUS_ACT_NONE = 0, JANUS_ACT_SILU = 1 } janus_act;
@@ -540,7 +540,8 @@ typedef enum janus_act { JANUS_ACT_NONE = 0, JANUS_ACT_SILU = 1 } janus_act;
  *   rows      rows of every array (>= 0, below 2^31)
  *   d         width, 1..8192 (wider: JANUS_EUNSUPPORTED)
  *   type      janus_type of x, b, r, n, the gate and their gradients
- *   eps       >= 0 (with 0, a row of zeros has no norm and gives NaN)
+ *   eps       >= 0 (with 0, a row of zeros has no norm and gives NaN, and so may one of values below 1e-18,
+ *             whose squares vanish in fp32)
  *   w_post, scale, w_pre  [d] fp32, or NULL
  *   gate      NULL; [rows, d] (one gate per row) with gate_off NULL; or [n_seq, d], one
  *             gate per sequence (structure), with
@@ -584,18 +585,19 @@ int janus_residual_norm_grad(const janus_norm* p /* host */, const void* dr, int
                              void* dgate, int64_t lddg, void* work, int64_t work_bytes, void* stream);
 
 /*
- * A whole expert layer for a few tokens (1..64), with the conventions of the training step's
- * layers: l = x router + beta in fp32, the top_k largest logits of a token (descending, lower
- * index first on ties), gates the softmax probabilities of the chosen (normalize = 1: divided by
- * their sum), y = sum_c g_c W_down^T SiLU(W_up^T x) of the chosen experts.
+ * A whole expert layer for a few tokens (1..64): l = x router + beta in fp32, the top_k largest logits of a
+ * token (descending, lower index first on ties), gates the softmax probabilities of the chosen (normalize = 1: divided
+ * by their sum), y = sum_c g_c W_down^T SiLU(W_up^T x) of the chosen experts.  One beta serves all tokens: the training
+ * step's layers, whose logits have a term of the token's species as well, are this for tokens of one species (or
+ * pair of species), with that term added to beta.
  *   d, d_hidden  widths, multiples of 16, at most 16384 and 65536
  *   n_experts    1..256;  top_k 1..min(n_experts, 8)
  *   type         janus_type of x, y, w_up and w_down
  *   router       [d, n_experts] fp32;  beta [n_experts] fp32 or NULL (-inf masks an expert out)
  *   w_up         [n_experts, d, d_hidden];  w_down [n_experts, d_hidden, d]; 16-byte aligned
- * x and y need rows that start on 16 bytes.  With 16-bit weights the hidden values enter the second product as three
- * bf16 each, whose sum they are.  Writes y [tokens, d], eid [tokens, top_k] int32 and gate
- * [tokens, top_k] fp32; expert ids are always valid and distinct.  A token whose logits are all -inf gets
+ * x and y need rows that start on 16 bytes.  With 16-bit weights the hidden values enter the second product as
+ * three bf16 each, whose sum they are (bits below 2^-133, bf16's least, are dropped).  Writes y [tokens, d], eid
+ * [tokens, top_k] int32 and gate [tokens, top_k] fp32; expert ids are always valid and distinct.  A token whose logits are all -inf gets
  * gates of zero and y = 0 (an expert with a gate of zero is left out, whatever its weights hold); one with a
  * logit of NaN or +inf gets gates and y of NaN.  Neither reaches other tokens.
  * The choice is exact up to the fp32 rounding of the logits.  y may not overlap x.
@@ -622,10 +624,10 @@ int janus_expert_layer(const janus_experts* p /* host */, const void* x, int64_t
  * Activations in 8 bits.  The columns of a row are cut into blocks of 32; a block holds int8
  * values q and one code byte c and stands for q 2^(c - 127).  The power of two is the least with
  * max|x| <= 127 2^(c - 127), but not below 2^-126; values are rounded to nearest, ties to even, so
- * each is off by at most max|x| / 127 of its block or 2^-127, whichever is more.  The largest values of a type may round to a power of two beyond
- * it (2^128, fp16: 2^16); janus_unpack_rows gives the type's largest finite value for that, janus_packed_wgrad takes 2^128 as
- * an infinity.  A block with an infinity or NaN gets c = 255 and q = 0 and reads as NaN; c = 0, which no block
- * gets, reads as zeros.
+ * each is off by at most max|x| / 127 of its block or 2^-127, whichever is more.  The largest values of a
+ * type may round to a power of two beyond it (2^128, fp16: 2^16); janus_unpack_rows gives the type's largest
+ * finite value for that, janus_packed_wgrad takes 2^128 as an infinity.  A block with an infinity or NaN gets
+ * c = 255 and q = 0 and reads as NaN; c = 0, which no block gets, reads as zeros.
  *   q [rows, d] int8, rows ldq apart;  code [rows, ceil(d / 32)] uint8, rows ldc apart; rows below 2^31, d
  *   at most 2^31 - 4097 (wider: JANUS_EUNSUPPORTED).
  * Columns of q between d and ldq, and of code behind the last block, are neither read into a result nor written.
@@ -647,9 +649,10 @@ int janus_unpack_rows(const int8_t* q, int64_t ldq, const uint8_t* code, int64_t
  *   G_g[p, c] = sum over the rows m of group g of X[m, p] B[m, c]
  * with X packed [rows, P], B [rows, Q] of `type`, G [n_groups, P, Q] fp32 and row_off [n_groups + 1]
  * int32 on the device, non-decreasing from 0 (row_off[n_groups] <= rows: rows behind the last group enter no
- * result).  1..1024 groups, rows at most 2^31 - 4097; groups without rows get zeros.  Every product is exact in fp32;
- * sums are held in fp32 and split over row chunks that are added in a fixed order.  An infinity or NaN of B reaches its own column,
- * a block of X that holds one its own rows.  Offsets that break these rules give wrong values but no access outside
+ * result).  1..1024 groups, rows at most 2^31 - 4097; groups without rows get zeros.  Products are
+ * exact in fp32 (of an fp32 B, which enters as three bf16, bits below 2^-133 are dropped); sums are held in fp32 and
+ * split over row chunks that are added in a fixed order.  An infinity or NaN of B reaches its own column, a block of X
+ * that holds one its own rows.  Offsets that break these rules give wrong values but no access outside
  * the arrays.  Rows of q and B that start on multiples of four bytes are read fastest; rows more than 262 144 bytes
  * apart may be refused (JANUS_EUNSUPPORTED), and sizes that one launch cannot hold are, by both functions.
  */

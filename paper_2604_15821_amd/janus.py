@@ -523,6 +523,8 @@ def grouped_gemm_noalloc(A, B, row_off, K, N, trans_b, out):
 
 
 # ------------------------------------------------------- operators around an expert block
+#
+# Calls on tensors' data, like the rest of this module: outputs carry no autograd history, gradients have calls of their own.
 
 ACT = {"none": 0, "silu": 1}
 
