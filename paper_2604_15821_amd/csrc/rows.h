@@ -54,20 +54,22 @@ __device__ __forceinline__ float row16_sum(float v) {
   return dpp_step<0x140>(v);   // row_mirror
 }
 
-// s = 1 / (1 + exp(-a)) and c = 1 - s, both to 7.6 units of 2^-24 of themselves at any a (SiLU(a) = a s to 8.6), down
-// into fp32's subnormal range.  exp(-|a|) = 2^n 2^f, where f is formed from the whole product |a| log2(e) in two
-// fused steps (the plain product would be rounded to |a| 2^-24, and so would the result), and the smaller of s and c is
-// e / (1 + e), without a difference.
+// s = 1 / (1 + exp(-a)) and c = 1 - s, the larger of them to 2.2 units of 2^-24 of itself and the smaller to 5.6, at any
+// a, down into fp32's subnormal range.  exp(-|a|) = 2^n 2^f, where f is formed from the whole product |a| log2(e) in two
+// fused steps (the plain product would be rounded to |a| 2^-24, and so would the result); the reciprocal of 1 + e takes
+// one step of Newton's with what the sum lost; and the smaller one is e / (1 + e), without a difference.  (With the
+// hardware's reciprocal of the rounded sum alone, SiLU of a value next to the middle of two bf16 went to the wrong one.)
 struct Sigmoid {
   float s, c;
 };
 __device__ __forceinline__ Sigmoid sigmoid(float a) {
-  constexpr float kLog2e = 1.44269502f, kRest = 1.92596299e-8f;   // log2(e) = their sum to 2^-50
-  const float x = fminf(fabsf(a), 150.0f);                        // exp(-150) is zero in fp32
+  constexpr float kLog2e = 1.44269502f, kRest = 1.92596299e-8f;     // log2(e) = their sum to 2^-50
+  const float x = __builtin_amdgcn_fmed3f(fabsf(a), 0.f, 150.0f);   // exp(-150) is zero in fp32
   const float n = rintf(-kLog2e * x);
   const float f = fmaf(-kRest, x, fmaf(-kLog2e, x, -n));
   const float e = ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
-  const float large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
+  const float t = 1.0f + e, lost = e - (t - 1.0f), r = __builtin_amdgcn_rcpf(t);
+  const float large = fmaf(r, fmaf(-lost, r, fmaf(-t, r, 1.0f)), r), small = e * large;
   return a < 0.f ? Sigmoid{small, large} : Sigmoid{large, small};
 }
 

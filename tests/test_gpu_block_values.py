@@ -16,10 +16,10 @@ def _dt(t):
 def test_unpacked_silu_far_from_zero():
     """SiLU and SiLU' of stored values from -104 to 104 in fp32.  With e = exp(-|a|): the hardware exponential is good
     to 2 E of itself on [2^-1/2, 2^1/2], where its argument is off by at most 2^-25 (0.4 E of the result), and the
-    power of two beside it is exact; 1 + e adds E to at most half of that, the reciprocal 2 E, and a product E each: 7.6 E for
-    s = 1 / (1 + e) or e / (1 + e), and for 1 - s, 8.6 E for a s.  SiLU' = s + (a s) (1 - s) takes 17.2 E of its second
-    term and E of the sum, the gradient E.  Below fp32's normal range a value is off by half a step of 2^-149, |a| times as
-    much where it is multiplied by a."""
+    power of two beside it is exact; at most half of that reaches 1 / (1 + e), whose rounding adds E: 2.2 E for the
+    larger of s and 1 - s, and with the error of e and a product 5.6 E for the smaller, 6.6 E for a s.  SiLU' = s (1 + a (1 - s))
+    takes 5.6 E of a s (1 - s), and of itself E for the sum, 5.6 E for s and E for either product.  Below fp32's normal
+    range a value is off by half a step of 2^-149, |a| times as much where it is multiplied by a."""
     import torch
     from paper_2604_15821_amd import janus
     banner("unpack silu far")
@@ -34,15 +34,15 @@ def test_unpacked_silu_far_from_zero():
     s, c = torch.where(a > 0, 1 / (1 + e), e / (1 + e)), torch.where(a > 0, e / (1 + e), 1 / (1 + e))
     small = (a.abs() + 2) * 2.0 ** -149
     want, dwant = a * s, g.double() * (s + a * s * c)
-    over = ((value.cpu().double() - want).abs() - (9 * E * want.abs() + small)).max().item()
+    over = ((value.cpu().double() - want).abs() - (7 * E * want.abs() + small)).max().item()
     assert over <= 0, over
-    dover = ((dx.cpu().double() - dwant).abs() - g.double() * (10 * E * s + 21 * E * (a * s * c).abs()) - small).max().item()
+    dover = ((dx.cpu().double() - dwant).abs() - 9 * E * dwant.abs() - 6 * E * g.double() * (a * s * c).abs() - small).max().item()
     assert dover <= 0, dover
 
 
 @pytest.mark.parametrize("tokens", [1, 20])
 def test_hidden_silu_far_from_zero(tokens):
-    """A hidden value of a large negative pre-activation, taken out by weights of one: 8.6 E for SiLU (see above) and
+    """A hidden value of a large negative pre-activation, taken out by weights of one: 6.6 E for SiLU (see above) and
     nothing for products with one and zero."""
     import torch
     from paper_2604_15821_amd import janus
@@ -59,7 +59,7 @@ def test_hidden_silu_far_from_zero(tokens):
     a = (x[:, :1] * up[0, :1]).double()             # as the kernel rounds the one product
     e = torch.exp(a)
     want = a * e / (1 + e)
-    over = ((y.cpu().double() - want).abs() - 9 * E * want.abs() - (a.abs() + 2) * 2.0 ** -149).max().item()
+    over = ((y.cpu().double() - want).abs() - 7 * E * want.abs() - (a.abs() + 2) * 2.0 ** -149).max().item()
     assert over <= 0, over
 
 
@@ -67,7 +67,7 @@ def test_hidden_silu_far_from_zero(tokens):
 @pytest.mark.parametrize("tokens", [1, 5, 64])
 def test_hidden_values_keep_their_bits(tokens, t):
     """Two hidden values near 1, 2^-15 apart, whose difference the second product forms with weights of 1 and -1.
-    Pre-activations are exact; a hidden value is off by 8.6 E of itself, its products are exact, and at most six
+    Pre-activations are exact; a hidden value is off by 3.2 E of itself (positive, see above), its products are exact, and at most six
     additions (three terms of each, zeros add nothing) cut off up to 2 E of the values' sum."""
     import torch
     from paper_2604_15821_amd import janus
@@ -90,7 +90,7 @@ def test_hidden_values_keep_their_bits(tokens, t):
     size = h.sum(1, keepdim=True)
     u = torch.finfo(dt).eps / 2
     tiny = 2.0 ** -25 if t == "f16" else 0.0
-    over = ((y.cpu().double() - want).abs() - (u * want.abs() + (9 + 12) * E * size * (1 + u) + tiny)).max().item()
+    over = ((y.cpu().double() - want).abs() - (u * want.abs() + (4 + 12) * E * size * (1 + u) + tiny)).max().item()
     assert over <= 0, over
 
 
@@ -253,3 +253,24 @@ def test_infinite_weights_give_what_the_formula_gives(tokens, t):
     bad = up.clone()
     bad[0, 4, 21] = float("inf")
     check(bad, down)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_unpacked_silu_next_to_a_rounding_border(t):
+    """SiLU and SiLU' of every value that 7 bits and a few powers of two give, in 16 bits: with an fp32 result off by
+    1.6 of its steps at most (3.2 E of a s for positive a), only what lies as near to the middle of two 16-bit values may
+    be rounded to the other one."""
+    import torch
+    from paper_2604_15821_amd import janus
+    banner("unpack silu borders", t)
+    q = torch.arange(1, 128, dtype=torch.int8).repeat(9).reshape(-1, 1)
+    code = (127 + torch.arange(-8, 1)).repeat_interleave(127).to(torch.uint8).reshape(-1, 1)
+    a = q.double() * (code.double() - 127).exp2()
+    want = a / (1 + torch.exp(-a))
+    got = janus.unpack_rows(janus.PackedRows(q.cuda(), code.cuda()), _dt(t), act="silu").cpu()
+    low, high = (want * (1 - 4 * E)).to(_dt(t)), (want * (1 + 4 * E)).to(_dt(t))
+    assert ((got == low) | (got == high)).all()
+    assert (got == want.to(_dt(t))).double().mean() > 0.998
+    if t == "bf16":
+        near = (a == 5.9375).nonzero()[0, 0]
+        assert got[near] == want[near].to(_dt(t))      # 1.18 fp32 steps below the middle
