@@ -5,8 +5,8 @@
 // 2^-126, so the rounding (to nearest, ties to even) is off by at most half of it: max|x| / 127, or 2^-127 where
 // that is more.  Code 255 stands for a block that held an infinity or NaN: all of it is NaN when read.
 // A power of two and seven bits fit bf16 exactly, so a product with a bf16 value is exact in fp32.
-// Packing and unpacking are bound by memory: 150 001 x 2048 fp32 to 8 bits 316 us (4.9 TB/s); SiLU and the gradient
-// through it in bf16 387 us (5.6 TB/s).
+// Packing and unpacking are bound by memory: 150 001 x 2048 fp32 to 8 bits 317 us (4.9 TB/s); SiLU and the gradient
+// through it in bf16 385 us (5.6 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -193,8 +193,9 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
 // Rows are cut into chunks, a group's longest first and given to the dies in turn, so that the tiles of a chunk
 // share its die's L2 and none runs long at the end.  A group's only chunk writes the gradient itself; else
 // each writes a partial and a second kernel adds them in order.
-// Measured, 150 001 rows in 64 ragged groups, 512 x 2048: bf16 0.40 ms (780 TFLOP/s; the matrix units are busy half of the
-// time, at the 1.7 GHz that power leaves), fp16 0.70 ms, fp32 1.05 ms (300 TFLOP/s, 900 of bf16 products).
+// Measured, 150 001 rows in 64 ragged groups, 512 x 2048, a whole call: bf16 0.39 ms (800 TFLOP/s; the product 0.36 ms at the
+// clock of an idle card, 0.42 once calls follow each other, its matrix units busy 48 % of the time in which a CU has
+// work), fp16 0.71 ms, fp32 1.06 ms (297 TFLOP/s, 890 of bf16 products).
 struct PackedChunk {
   int group, r0, r1, alone;
 };
