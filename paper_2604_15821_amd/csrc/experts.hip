@@ -4,9 +4,9 @@
 //   g = softmax(l) of the chosen (normalize: divided by their sum)
 //   y = sum_c g_c W2_c^T SiLU(W1_c^T x)
 //
-// Bound by the chosen experts' weights, which are read once: 48 tokens, 32 experts of 1024 x 4096 bf16, 136 us for 537 MB
-// from memory (the products 4.5 and 3.9 TB/s; 115 us where a part is still in the last-level cache), and for a token or
-// two by the chain of launches: 19 us for 17 MB (512 x 2048 fp32).
+// Bound by the chosen experts' weights, which are read once: 48 tokens, 32 experts of 1024 x 4096 bf16, 114 to 136 us for 537 MB,
+// by where the weights lie in memory (the products 4.3 to 5.2 and 3.3 to 5.2 TB/s), and for a token or two by the chain of
+// launches: 19 us for 17 MB (512 x 2048 fp32).
 #include <algorithm>
 #include <type_traits>
 
