@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(PackShape s, const int
 // Rows are cut into chunks, a group's longest first and given to the dies in turn, so that the tiles of a chunk
 // share its die's L2 and none runs long at the end.  A group's only chunk writes the gradient itself; else
 // each writes a partial and a second kernel adds them in order.
-// Measured, 150 001 rows in 64 ragged groups, 512 x 2048, a whole call: bf16 0.39 ms (800 TFLOP/s; the product 0.36 ms at the
+// Measured, 150 001 rows in 64 ragged groups, 512 x 2048, a whole call: bf16 0.39 ms (800 TFLOP/s; the product 0.36 at the
 // clock of an idle card, 0.42 once calls follow each other, its matrix units busy 48 % of the time in which a CU has
 // work), fp16 0.71 ms, fp32 1.06 ms (297 TFLOP/s, 890 of bf16 products).
 struct PackedChunk {
@@ -626,8 +626,8 @@ static unsigned pack_grid(const PackShape& s) {
   return (unsigned)(need < 8192 ? need : 8192);
 }
 // Unpacking: workgroups that take several rows each spare a short call the set-up per row (200 000 x 200 bf16, SiLU and
-// gradient, 48 us with 8192 workgroups, 58 with as many as rows allow); in a long call they drift apart over the memory
-// (150 001 x 2048: 449 us with 8192, 396 with 32 768, 384 with 65 536).
+// gradient, 52 us with 8192 workgroups, 60 with as many as rows allow); in a long call they drift apart over the memory
+// (150 001 x 2048: 439 us with 8192, 401 with 32 768, 386 with 65 536).
 static unsigned unpack_grid(const PackShape& s) {
   const long long need = (s.rows + 256 / s.tpr - 1) / (256 / s.tpr), most = need < 32768 ? 8192 : 65536;
   return (unsigned)(need < most ? need : most);
